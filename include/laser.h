@@ -54,6 +54,9 @@ enum {
                               STRICT or RELAXED accepts                                    */
 };
 
+/* Types of the rows that laser_kv_append takes. */
+enum { LASER_DTYPE_BF16 = 0, LASER_DTYPE_F32 = 1 };
+
 typedef struct laser_pool laser_pool;
 typedef struct laser_model laser_model;
 typedef struct laser_kv laser_kv;
@@ -230,6 +233,19 @@ laser_status laser_model_free(laser_model* m);
 laser_status laser_kv_create(const laser_model* m, int32_t max_seqs, int64_t n_pages,
                              laser_kv** out);
 laser_status laser_kv_free(laser_kv* kv);
+/* The same in 4 bits: 5 bits a value with its scales, 0.31 of the bf16 cache's memory and traffic.
+ * Per token, head and group of 32 features there are codes 0 .. 15, a scale s and a zero z in bf16:
+ *   s = bf16((max - min) / 15), 0 where that is below 2^-100;  z = bf16(min - 16 s)
+ *   code = rint((x - z) / s) - 16, clamped to 0 .. 15 (0 where s = 0), stands for bf16(s (16 + code) + z)
+ * (NaN is stored as 0 and magnitudes above 2^124 as 2^124: the cache holds finite numbers alone).
+ * Every call that takes a cache takes either form: laser_verify_step, _tree, laser_verify_accept and
+ * laser_generate write and read it, laser_kv_import rounds to it, laser_kv_export gives the bf16
+ * numbers that it stands for, and laser_accept_tree / laser_kv_compact_path move codes as they are.
+ * Logits are those of a model whose keys and values are rounded this way; 2048 sequences a step at most.
+ * The first such cache of a model also allocates fp32 rows for a layer's projections (a model that did
+ * not create the cache does so in its first step over it, which must not be under stream capture).
+ * Errors: UNSUPPORTED (head_dim other than 64 and 128, a precise model), INVALID_ARG, OOM. */
+laser_status laser_kv_create_int4(laser_model* m, int32_t max_seqs, int64_t n_pages, laser_kv** out);
 /* host int32[max_seqs * pages_per_seq]: physical page of each logical page; every entry
  * must be unique and < n_pages.  Synchronous. */
 laser_status laser_kv_set_page_table(laser_kv* kv, const int32_t* table);
@@ -250,6 +266,50 @@ laser_status laser_kv_import(laser_kv* kv, int32_t seq, int32_t layer, int32_t p
                              const void* k, const void* v, void* stream);
 laser_status laser_kv_export(const laser_kv* kv, int32_t seq, int32_t layer, int32_t pos0,
                              int32_t n, void* k, void* v, void* stream);
+
+/* ---- The cache by itself: rows in, attention out --------------------------------------------
+ * What laser_verify_step does around the projections of one layer, for callers with a forward of
+ * their own.  The rows of sequence b are 0 .. n_rows[b]-1 (clamped to 0 .. rows); row i has the
+ * position len + i and goes to cache slot len + i.  With parents (dev int32[B, rows], as
+ * laser_verify_step_tree; rows <= 64) its position is len + depth(i).  Committed lengths are read
+ * and not changed.  seq_ids must be distinct.  Calls on one cache must not overlap on the GPU.
+ *
+ * laser_kv_append: q and k are rotated (rotate-half pairing, the model's rope_theta, angles in 64
+ * bits), k and v go to the cache, of either form.
+ *   q, k, v  dev rows b * rows + i of n_heads (q) or n_kv_heads times head_dim elements of `dtype`,
+ *            q_stride, k_stride, v_stride elements apart: three arrays, or parts of a fused
+ *            projection's rows.  q may be NULL, together with q_out.  Rows aligned to four elements are
+ *            read fastest.
+ *   q_out    dev bf16[B, rows, n_heads, head_dim]: the rotated queries
+ *   k_out, v_out  dev bf16[B, rows, n_kv_heads, head_dim], each may be NULL: the numbers that the
+ *            cache now holds
+ * Rows that are not active are not read, cached or written.  rows * B <= 2^31 - 1 (prompts are
+ * appended as rows too).  Asynchronous on `stream`.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim other than 64 and 128); found on the device and
+ * reported by laser_kv_check, the sequence's rows then left out: INVALID_ARG (a bad sequence id or
+ * parent; the rows behind a bad parent count their depth from it), CAPACITY (a sequence would outgrow its pages). */
+laser_status laser_kv_append(laser_kv* kv, int32_t layer, const int32_t* seq_ids, const int32_t* parents,
+                             const int32_t* n_rows, int32_t B, int32_t rows, int32_t dtype,
+                             const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, void* q_out, void* k_out, void* v_out,
+                             void* stream);
+/* laser_attend_int4: attention of the rows over a 4-bit cache that already has their own keys and
+ * values (laser_kv_append): out = softmax(q k / sqrt(head_dim)) v over the sequence's len tokens and
+ * rows 0 .. i (with parents: row i's ancestors and itself), heads h * n_kv_heads / n_heads grouped.
+ * bf16 products with fp32 sums; probabilities enter the second product as bf16.
+ *   q    dev bf16 rows of n_heads * head_dim, q_stride elements apart, 16-byte aligned rows
+ *   out  dev bf16 rows likewise, out_stride apart, 4-byte aligned; rows that are not active are left
+ *        as they are
+ * The work is divided evenly over the SMs whatever the lengths.  It keeps partial results in memory of
+ * the cache's.  Asynchronous on `stream`.
+ * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 2048); on the device as above,
+ * and TIMEOUT. */
+laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int32_t* seq_ids, const int32_t* parents,
+                               const int32_t* n_rows, int32_t B, int32_t rows, const void* q, int64_t q_stride,
+                               void* out, int64_t out_stride, void* stream);
+/* Synchronises `stream` and returns the first device-side error that the calls on the cache itself
+ * recorded since the last check, clearing it (those of a model's steps: laser_check). */
+laser_status laser_kv_check(laser_kv* kv, void* stream);
 
 /* ---- Verify forward: q_i = M(x_<=t, x~_<i), i = 1..K+1, Eq. 3 / Eq. 6 -------------------
  * One forward of the decoder over the rows of B sequences.  Row i of sequence b is
@@ -289,6 +349,37 @@ laser_status laser_check(laser_model* m, void* stream);
  * summed device time and the number of launches of one class since the previous read. */
 laser_status laser_profile_enable(laser_model* m, int32_t on);
 laser_status laser_profile_read(laser_model* m, int32_t cls, double* ms, int64_t* launches);
+
+/* ---- Logits between verify and acceptance ----------------------------------------------------
+ * Penalties, biases and grammar masks on the logits of a step.  A draft is on the path of the rows
+ * that follow it, so each row counts its own.  For row i of sequence b and token v, with n = how
+ * often v occurs in the generated part of the text and on the path (rows 1 .. i; with parents row
+ * i's ancestors and itself; row 0, the pending token, is the text's last):
+ *   x = logit;  v in the text or on the path:  x = x > 0 ? x / repetition[b] : x * repetition[b]
+ *   x = (x - frequency[b] * n) - presence[b] (if n > 0);  x = x + bias_b(v);  v not allowed: x = -inf
+ *   logits, out  dev fp32[B, rows, V]; out may be logits itself (other overlaps are refused).  Rows that
+ *            are not active are left as they are
+ *   tokens, parents (or NULL), n_rows  as for laser_verify_step(_tree), rows = K + 1 <= 64
+ *   hist, hist_len, hist_stride  the texts as laser_draft_temp takes them, pending token included
+ *            (NULL: no text); prompt_len dev int32[B]: how much of each is prompt, which counts for the
+ *            repetition penalty alone (NULL: all of it is generated)
+ *   repetition, frequency, presence  dev fp32[B], each may be NULL (1, 0, 0)
+ *   bias_offsets dev int32[B+1], bias_ids int32, bias_values fp32: the biases of sequence b are
+ *            entries bias_offsets[b] .. bias_offsets[b+1]-1; those of one token add up in the
+ *            list's order.  NULL, all three: none
+ *   allowed  dev words of 32 tokens, bit v % 32 of word v / 32 set = allowed; the mask of a row starts
+ *            at b * mask_seq_stride + i * mask_row_stride words (row stride 0: one mask a sequence).
+ *            NULL: all are allowed
+ * Token ids outside [0, V), in the text, the drafts and the biases, are ignored.  A row of which the mask
+ * leaves nothing is -inf throughout.  Asynchronous on `stream`; no scratch memory.
+ * Errors: INVALID_ARG (rows outside 1 .. 64, an overlap, strides shorter than a mask). */
+laser_status laser_adjust_logits(const float* logits, const int32_t* tokens, const int32_t* parents,
+                                 const int32_t* n_rows, const int32_t* hist, const int32_t* hist_len,
+                                 int64_t hist_stride, const int32_t* prompt_len, const float* repetition,
+                                 const float* frequency, const float* presence, const int32_t* bias_offsets,
+                                 const int32_t* bias_ids, const float* bias_values, const uint32_t* allowed,
+                                 int64_t mask_seq_stride, int64_t mask_row_stride, int32_t B, int32_t rows,
+                                 int32_t V, float* out, void* stream);
 
 /* ---- Acceptance and commit (Section 2.1, Section 3.4, Eq. 4 / Eq. 7 / Eq. 8) ------------
  * Drafts are verified in order against rows 0.. of the logits; n_accept[b] = drafts that

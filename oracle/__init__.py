@@ -10,7 +10,9 @@ restatement of what the decoding loop computes, written from the paper:
 * ``accept``    - greedy verification (Eq. 4) and Relaxed Verification (Eq. 8)
   plus the ablation variants of Section 4.3.2, in fp64,
 * ``generate``  - the Draft-Then-Verify loop of Section 2.1 and plain
-  autoregressive greedy decoding (Eq. 1).
+  autoregressive greedy decoding (Eq. 1),
+* ``int4``      - the 4-bit cache's format, rows stored in it and attention over it,
+* ``adjust``    - penalties, biases and masks on a step's logits.
 
 It shares no code with the CUDA library, never imports it, and must only be
 used by the tests, by the smoke check and by the benchmark's CPU baseline.

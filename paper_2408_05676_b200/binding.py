@@ -63,6 +63,7 @@ EXPORTS = ["laser_version", "laser_last_error", "laser_launch_count", "laser_poo
            "laser_kv_get_len", "laser_kv_reset", "laser_kv_set_len_dev", "laser_kv_import", "laser_kv_export",
            "laser_verify_step", "laser_verify_step_tree", "laser_check", "laser_profile_enable", "laser_profile_read", "laser_accept_commit", "laser_accept_commit_noalloc", "laser_accept_tree", "laser_kv_compact_path",
            "laser_verify_accept",
+           "laser_kv_create_int4", "laser_kv_append", "laser_attend_int4", "laser_kv_check", "laser_adjust_logits",
            "laser_selftest_wait", "laser_selftest_peers", "laser_group_kmeans", "laser_generate"]
 
 lib.laser_version.restype = C.c_char_p
@@ -111,6 +112,10 @@ _declare("laser_draft", 4, _I, _P, _P, _P, _P, _P)
 _declare("laser_draft_tree", 6, C.c_int64, _I, _P, _P, _P, _P, _P, _P)
 _declare("laser_make_rows", 3, _I, _I, _P, _P, _P)
 _declare("laser_make_rows_tree", 4, _I, _I, _P, _P, _P, _P)
+_L = C.c_int64
+_declare("laser_kv_append", 1, _I, _P, _P, _P, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _P, _P, _P)
+_declare("laser_attend_int4", 1, _I, _P, _P, _P, _I, _I, _P, _L, _P, _L, _P)
+_declare("laser_adjust_logits", 6, _L, *[_P] * 8, _L, _L, _I, _I, _I, _P, _P)
 _declare("laser_accept_commit", 5, _I, _I, _P, _P, _P, _P, _P)
 _declare("laser_accept_commit_noalloc", 5, _I, _I, _P, _P, _P, _P, _P)
 
@@ -315,6 +320,68 @@ def kv_create(model: Model, max_seqs: int, n_pages: int) -> KV:
     return KV(h, model, max_seqs, n_pages)
 
 
+def kv_create_int4(model: Model, max_seqs: int, n_pages: int) -> KV:
+    """laser_kv_create_int4: the cache in 4 bits a value, for all that takes a cache."""
+    h = C.c_void_p()
+    _chk(lib.laser_kv_create_int4(model.handle, C.c_int32(max_seqs), C.c_int64(n_pages), C.byref(h)))
+    return KV(h, model, max_seqs, n_pages)
+
+
+def _rows_at(t: torch.Tensor, dtype, B: int, rows: int, width: int):
+    """Address and row stride (in elements) of [B, rows, ..] rows of `width` adjacent elements on the GPU, which may lie apart."""
+    assert t.is_cuda and t.dtype == dtype, (t.device, t.dtype, dtype)
+    sizes, strides = t.shape, t.stride()
+    assert sizes[0] == B and sizes[1] == rows, (tuple(sizes), B, rows)
+    if len(sizes) == 3:
+        assert sizes[2] == width and strides[2] == 1, (tuple(sizes), strides, width)
+    else:
+        assert len(sizes) == 4 and sizes[2] * sizes[3] == width and strides[3] == 1 and strides[2] == sizes[3], (tuple(sizes), strides, width)
+    ld = strides[1] if rows > 1 else strides[0] if B > 1 else width
+    assert B == 1 or strides[0] == rows * ld, "rows must be evenly spaced"
+    return t.data_ptr(), ld
+
+
+def kv_append(kv: KV, layer: int, seq_ids, n_rows, k, v, q=None, parents=None, q_out=None, k_out=None, v_out=None, stream=None):
+    """laser_kv_append: q [B, rows, n_heads * head_dim] (or split into heads), k and v likewise with n_kv_heads, bf16 or fp32, in rows
+    that may be parts of longer ones.  Returns q_out, the rotated queries (None without q); k_out and v_out (optional) receive what
+    the cache now holds."""
+    cfg = kv.model.cfg
+    H, Hkv, dh = cfg["n_heads"], cfg["n_kv_heads"], cfg["head_dim"]
+    B, rows = k.shape[0], k.shape[1]
+    assert k.dtype in (torch.bfloat16, torch.float32), k.dtype
+    assert seq_ids.shape == (B,) and n_rows.shape == (B,) and (parents is None or parents.shape == (B, rows))
+    (ka, ks), (va, vs) = _rows_at(k, k.dtype, B, rows, Hkv * dh), _rows_at(v, k.dtype, B, rows, Hkv * dh)
+    qa, qs = (0, 0) if q is None else _rows_at(q, k.dtype, B, rows, H * dh)
+    if q is not None and q_out is None:
+        q_out = torch.empty(B, rows, H, dh, dtype=torch.bfloat16, device=k.device)
+    assert q_out is None or q_out.numel() == B * rows * H * dh
+    assert all(t is None or t.numel() == B * rows * Hkv * dh for t in (k_out, v_out))
+    out = [0 if t is None else _at(t, torch.bfloat16) for t in (q_out, k_out, v_out)]
+    _chk(lib.laser_kv_append(kv.handle, layer, _at(seq_ids, torch.int32), None if parents is None else _at(parents, torch.int32),
+                             _at(n_rows, torch.int32), B, rows, 0 if k.dtype == torch.bfloat16 else 1, qa, qs, ka, ks, va, vs, *out,
+                             _stream_at(stream)))
+    return q_out
+
+
+def attend_int4(kv: KV, layer: int, seq_ids, n_rows, q, parents=None, out=None, stream=None) -> torch.Tensor:
+    """laser_attend_int4: q bf16 [B, rows, n_heads, head_dim] (or [.., n_heads * head_dim]), rows that may be parts of longer ones, as
+    may those of out."""
+    cfg = kv.model.cfg
+    width = cfg["n_heads"] * cfg["head_dim"]
+    B, rows = q.shape[0], q.shape[1]
+    assert seq_ids.shape == (B,) and n_rows.shape == (B,) and (parents is None or parents.shape == (B, rows))
+    if out is None:
+        out = torch.empty(B, rows, cfg["n_heads"], cfg["head_dim"], dtype=torch.bfloat16, device=q.device)
+    (qa, qs), (oa, os_) = _rows_at(q, torch.bfloat16, B, rows, width), _rows_at(out, torch.bfloat16, B, rows, width)
+    _chk(lib.laser_attend_int4(kv.handle, layer, _at(seq_ids, torch.int32), None if parents is None else _at(parents, torch.int32),
+                               _at(n_rows, torch.int32), B, rows, qa, qs, oa, os_, _stream_at(stream)))
+    return out
+
+
+def kv_check(kv: KV, stream=None) -> None:
+    _chk(lib.laser_kv_check(kv.handle, _stream(stream)))
+
+
 def kv_set_page_table(kv: KV, table: np.ndarray) -> None:
     t = np.ascontiguousarray(table, dtype=np.int32)
     _chk(lib.laser_kv_set_page_table(kv.handle, _ptr(t)))
@@ -410,6 +477,32 @@ def selftest_peers(model: Model, wait_cycles: int = 200000) -> int:
     left = C.c_int32()
     _chk(lib.laser_selftest_peers(model.handle, C.c_int32(wait_cycles), C.byref(left)))
     return left.value
+
+
+def adjust_logits(logits, tokens, n_rows, hist=None, hist_len=None, prompt_len=None, penalties=(None, None, None), bias=None, allowed=None,
+                  parents=None, out=None, stream=None) -> torch.Tensor:
+    """laser_adjust_logits: penalties = (repetition, frequency, presence), fp32 [B] or None each; bias = (offsets int32 [B + 1], ids int32,
+    values fp32) or None; allowed int32 [B, rows or 1, words of 32 tokens] or None.  out may be logits."""
+    B, R, V = logits.shape
+    if out is None:
+        out = torch.empty_like(logits)
+    assert tokens.shape == (B, R) and out.shape == logits.shape and n_rows.shape == (B,) and (parents is None or parents.shape == (B, R))
+    assert (hist is None) == (hist_len is None), "hist and hist_len go together"
+    i32 = lambda t: None if t is None else _at(t, torch.int32)
+    f32 = lambda t: None if t is None else _at(t, torch.float32)
+    assert hist is None or (hist.dim() == 2 and hist.shape[0] == B and hist_len.shape == (B,))
+    assert all(t is None or t.shape == (B,) for t in (prompt_len, *penalties))
+    off, ids, val = bias if bias is not None else (None, None, None)
+    assert off is None or (off.shape == (B + 1,) and ids.shape == val.shape)
+    ss = rs = 0
+    if allowed is not None:
+        words = -(-V // 32)
+        assert allowed.dim() == 3 and allowed.shape[0] == B and allowed.shape[1] in (1, R) and allowed.shape[2] >= words, tuple(allowed.shape)
+        ss, rs = allowed.shape[1] * allowed.shape[2], allowed.shape[2] if allowed.shape[1] == R else 0
+    _chk(lib.laser_adjust_logits(_at(logits, torch.float32), _at(tokens, torch.int32), i32(parents), _at(n_rows, torch.int32), i32(hist),
+                                 i32(hist_len), 0 if hist is None else hist.shape[1], i32(prompt_len), *[f32(t) for t in penalties],
+                                 i32(off), i32(ids), f32(val), i32(allowed), ss, rs, B, R, V, _at(out, torch.float32), _stream_at(stream)))
+    return out
 
 
 def accept_commit_noalloc(kv: Optional[KV], seq_ids, logits, tokens, n_rows, params: Params, out, stream=None):

@@ -9,7 +9,7 @@
 // last CTA of a sequence to finish walks the tree.  Reductions have a fixed shape.
 #include <algorithm>
 
-#include "state.cuh"
+#include "model.cuh"
 #include "verdict.cuh"
 
 namespace laser {
@@ -138,6 +138,7 @@ LASER_API laser_status laser_kv_compact_path(laser_kv* kv, const int32_t* seq_id
   LASER_REQUIRE(B >= 0 && row_stride >= 1, "B = %d, row_stride = %d", B, row_stride);
   LASER_REQUIRE(kv->head_dim % 8 == 0, "head_dim = %d is not a multiple of 8", kv->head_dim);
   if (B == 0) return LASER_OK;
+  if (kv->pages4) return compact_path_q4(kv, seq_ids, path_rows, n_accept, B, row_stride, as_stream(stream));
   const int capacity = int(std::min<int64_t>(kv->capacity_tokens(), INT32_MAX));
   LASER_CUDA(launch_overlapped(compact_path_kernel, dim3(unsigned(B), unsigned(kv->n_layers)), 128, 0, as_stream(stream),
       kv->pages, kv->layer_elems(), kv->page_elems(), kv->page_table, kv->pages_per_seq, kv->n_kv_heads, kv->head_dim,

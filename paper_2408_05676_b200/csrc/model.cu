@@ -281,6 +281,9 @@ laser_status fuse_rows(laser_model* m, const void* const* pieces, const size_t* 
   return LASER_OK;
 }
 
+// Rows for a layer's projections, which a step over a 4-bit cache keeps in fp32 until they are rotated and stored.
+laser_status qkv_rows(laser_model* m) { return m->qkv ? LASER_OK : model_alloc(m, &m->qkv, size_t(m->R_cap) * m->dqkv); }
+
 }  // namespace
 }  // namespace laser
 
@@ -409,8 +412,30 @@ LASER_API laser_status laser_model_create(const laser_model_cfg* cfg, const lase
 
 LASER_API laser_status laser_kv_free(laser_kv* kv) {
   if (!kv) return LASER_OK;
-  cudaFree(kv->pages); cudaFree(kv->page_table); cudaFree(kv->seq_len);
+  cudaFree(kv->pages); cudaFree(kv->pages4); cudaFree(kv->page_table); cudaFree(kv->seq_len);
+  cudaFree(kv->inv_freq); cudaFree(kv->status); cudaFree(kv->attn_part); cudaFree(kv->attn_arrived);
   delete kv;
+  return LASER_OK;
+}
+
+// The parts that caches of both forms have.
+static laser_status kv_open(const laser_model* m, int32_t max_seqs, int64_t n_pages, laser_kv* kv) {
+  kv->n_layers = m->cfg.n_layers; kv->n_kv_heads = m->cfg.n_kv_heads; kv->head_dim = m->cfg.head_dim; kv->n_heads = m->cfg.n_heads;
+  kv->max_seqs = max_seqs; kv->n_pages = n_pages;
+  kv->pages_per_seq = int32_t(std::min<int64_t>(n_pages / max_seqs, 1 << 20));
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->page_table), size_t(max_seqs) * kv->pages_per_seq * 4));
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->seq_len), size_t(max_seqs) * 4));
+  LASER_CUDA(cudaMemset(kv->seq_len, 0, size_t(max_seqs) * 4));
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->status), 4));
+  LASER_CUDA(cudaMemset(kv->status, 0, 4));
+  std::vector<double> inv_freq(size_t(kv->head_dim) / 2);
+  for (size_t j = 0; j < inv_freq.size(); ++j) inv_freq[j] = std::pow(double(m->cfg.rope_theta), -2.0 * double(j) / double(kv->head_dim));
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->inv_freq), inv_freq.size() * 8));
+  LASER_CUDA(cudaMemcpy(kv->inv_freq, inv_freq.data(), inv_freq.size() * 8, cudaMemcpyHostToDevice));
+  std::vector<int32_t> table(size_t(max_seqs) * kv->pages_per_seq);
+  for (int s = 0; s < max_seqs; ++s)
+    for (int j = 0; j < kv->pages_per_seq; ++j) table[size_t(s) * kv->pages_per_seq + j] = j * max_seqs + s;
+  LASER_CUDA(cudaMemcpy(kv->page_table, table.data(), table.size() * 4, cudaMemcpyHostToDevice));
   return LASER_OK;
 }
 
@@ -419,25 +444,39 @@ LASER_API laser_status laser_kv_create(const laser_model* m, int32_t max_seqs, i
   LASER_REQUIRE(max_seqs >= 1 && n_pages >= max_seqs, "max_seqs = %d, n_pages = %lld", max_seqs, (long long)n_pages);
   laser_kv* kv = new laser_kv();
   struct Guard { laser_kv* p; ~Guard() { if (p) laser_kv_free(p); } } guard{kv};
-  kv->n_layers = m->cfg.n_layers; kv->n_kv_heads = m->cfg.n_kv_heads; kv->head_dim = m->cfg.head_dim;
-  kv->max_seqs = max_seqs; kv->n_pages = n_pages;
-  kv->pages_per_seq = int32_t(std::min<int64_t>(n_pages / max_seqs, 1 << 20));
+  LASER_TRY(kv_open(m, max_seqs, n_pages, kv));
   const size_t elems = std::max<size_t>(1, size_t(kv->n_layers) * kv->layer_elems());
   LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->pages), elems * sizeof(__nv_bfloat16)));
   // masked keys still enter P*V with weight 0, so the pages must never hold NaN/Inf patterns
   LASER_CUDA(cudaMemset(kv->pages, 0, elems * sizeof(__nv_bfloat16)));
-  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->page_table), size_t(max_seqs) * kv->pages_per_seq * 4));
-  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->seq_len), size_t(max_seqs) * 4));
-  LASER_CUDA(cudaMemset(kv->seq_len, 0, size_t(max_seqs) * 4));
-  std::vector<int32_t> table(size_t(max_seqs) * kv->pages_per_seq);
-  for (int s = 0; s < max_seqs; ++s)
-    for (int j = 0; j < kv->pages_per_seq; ++j) table[size_t(s) * kv->pages_per_seq + j] = j * max_seqs + s;
-  LASER_CUDA(cudaMemcpy(kv->page_table, table.data(), table.size() * 4, cudaMemcpyHostToDevice));
   const uint64_t map_rows = uint64_t(kv->n_layers) * uint64_t(n_pages) * 2 * kv->n_kv_heads * 16;
   if (kv->head_dim % 64 == 0 && map_rows > 0 && map_rows < (uint64_t(1) << 31)) {
     LASER_TRY(encode_bf16_2d(&kv->pages_map, kv->pages, map_rows, uint64_t(kv->head_dim), 16));
     kv->has_pages_map = true;
   }
+  guard.p = nullptr;
+  *out = kv;
+  return LASER_OK;
+}
+
+LASER_API laser_status laser_kv_create_int4(laser_model* m, int32_t max_seqs, int64_t n_pages, laser_kv** out) {
+  LASER_REQUIRE(m && out, "null argument");
+  LASER_REQUIRE(max_seqs >= 1 && n_pages >= max_seqs, "max_seqs = %d, n_pages = %lld", max_seqs, (long long)n_pages);
+  if (m->cfg.head_dim != 64 && m->cfg.head_dim != 128) { set_error("head_dim = %d (a 4-bit cache needs 64 or 128)", m->cfg.head_dim); return LASER_ERR_UNSUPPORTED; }
+  if (m->precise) { set_error("a precise model keeps its cache in bf16"); return LASER_ERR_UNSUPPORTED; }
+  LASER_TRY(qkv_rows(m));
+  laser_kv* kv = new laser_kv();
+  struct Guard { laser_kv* p; ~Guard() { if (p) laser_kv_free(p); } } guard{kv};
+  LASER_TRY(kv_open(m, max_seqs, n_pages, kv));
+  const size_t bytes = std::max<size_t>(16, size_t(kv->n_layers) * kv->layer_bytes4());
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->pages4), bytes));
+  LASER_CUDA(cudaMemset(kv->pages4, 0, bytes));      // scales and zeros of 0: finite, as masked tokens have to be
+  int dev = 0;
+  LASER_CUDA(cudaGetDevice(&dev));
+  LASER_CUDA(cudaDeviceGetAttribute(&kv->attn_ctas, cudaDevAttrMultiProcessorCount, dev));
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->attn_part), attention_int4_part_floats(kv->head_dim, kv->attn_ctas) * sizeof(float)));
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->attn_arrived), size_t(kv->attn_ctas) * sizeof(int32_t)));
+  LASER_CUDA(cudaMemset(kv->attn_arrived, 0, size_t(kv->attn_ctas) * sizeof(int32_t)));
   guard.p = nullptr;
   *out = kv;
   return LASER_OK;
@@ -498,6 +537,7 @@ static laser_status kv_copy(const laser_kv* kv, int32_t seq, int32_t layer, int3
   LASER_REQUIRE(seq >= 0 && seq < kv->max_seqs && layer >= 0 && layer < kv->n_layers, "seq / layer out of range");
   LASER_REQUIRE(pos0 >= 0 && n >= 0 && int64_t(pos0) + n <= kv->capacity_tokens(), "positions [%d, %d) outside the sequence's pages", pos0, pos0 + n);
   if (n == 0) return LASER_OK;
+  if (kv->pages4) return kv_copy_q4(kv, seq, layer, pos0, n, k, v, to_pages != 0, as_stream(stream));
   const size_t total = size_t(n) * kv->n_kv_heads * kv->head_dim;
   kv_copy_kernel<<<unsigned(std::min<size_t>(ceil_div<size_t>(total, 256), 4096)), 256, 0, as_stream(stream)>>>(
       kv->pages + size_t(layer) * kv->layer_elems(), kv->page_elems(), kv->page_table + size_t(seq) * kv->pages_per_seq,
@@ -613,6 +653,12 @@ static laser_status verify_impl(laser_model* m, laser_kv* kv, const int32_t* seq
                 "B = %d sequences of %d rows outside the model's %d rows (max_batch = %d)", B, Rs, max_rows, m->cfg.max_batch);
   LASER_REQUIRE(kv->n_layers == m->cfg.n_layers && kv->n_kv_heads == m->cfg.n_kv_heads && kv->head_dim == m->cfg.head_dim,
                 "cache was created for another model shape");
+  const bool q4 = kv->pages4 != nullptr;
+  if (q4) {
+    if (m->precise) { set_error("a precise model needs a bf16 cache"); return LASER_ERR_UNSUPPORTED; }
+    if (B > attention_int4_max_groups()) { set_error("B = %d sequences over a 4-bit cache (at most %d)", B, attention_int4_max_groups()); return LASER_ERR_CAPACITY; }
+    LASER_TRY(qkv_rows(m));
+  }
   // the LM head stores four logits at a time
   LASER_REQUIRE((reinterpret_cast<uintptr_t>(logits) & 15) == 0, "logits must be 16-byte aligned");
   cudaStream_t stream = as_stream(stream_);
@@ -632,7 +678,7 @@ static laser_status verify_impl(laser_model* m, laser_kv* kv, const int32_t* seq
   count_launch();
   const bool use_tma_attn = attention_tma_supported(m, kv);
   const size_t attn_smem = (size_t(dh) + size_t(capacity) + 8) * sizeof(float);
-  if (!use_tma_attn && attn_smem > 48 * 1024) {
+  if (!q4 && !use_tma_attn && attn_smem > 48 * 1024) {
     LASER_REQUIRE(attn_smem <= 200 * 1024, "KV capacity of %d tokens per sequence exceeds the attention kernel's limit", capacity);
     LASER_CUDA(cudaFuncSetAttribute(attention_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(attn_smem)));
   }
@@ -645,10 +691,20 @@ static laser_status verify_impl(laser_model* m, laser_kv* kv, const int32_t* seq
   base.out_split = m->precise ? 1 : 0;
   int norm_tiles = 1;  // tile planes holding the sums of squares of the current residual
   for (int l = 0; l < c.n_layers; ++l) {
-    __nv_bfloat16* pages_l = kv->pages + size_t(l) * kv->layer_elems();
+    __nv_bfloat16* pages_l = q4 ? nullptr : kv->pages + size_t(l) * kv->layer_elems();
     // Of the last layer a prompt leaves its keys and values alone: their projections are all that it runs.
     const bool kv_alone = start && l == c.n_layers - 1;
-    {  // QKV projection of the normalised residual; rotary embedding; Q store; cache write
+    if (q4) {  // QKV projection of the normalised residual to fp32 rows; rotary embedding, Q store and 4-bit cache write
+      GemmEpilogue e = base;
+      const int width = kv_alone ? 2 * m->dkv : m->dqkv;
+      e.sumsq_in = m->sumsq; e.sumsq_in_tiles = norm_tiles;
+      e.out = m->qkv; e.ldo = width; e.R_store = R;
+      {
+        ProfScope ps(m, 0, stream);
+        LASER_TRY(gemm_fused(m, m->xn, m->wqkv[l] + (kv_alone ? size_t(m->dq) * d : 0), Rp, width, d, EPI_PLAIN, e, stream));
+      }
+      LASER_TRY(append_step_rows(m, kv, l, m->qkv, width, !kv_alone, R, stream));
+    } else {  // the same; rotary embedding, Q store and cache write in the epilogue
       GemmEpilogue e = base;
       e.sumsq_in = m->sumsq; e.sumsq_in_tiles = norm_tiles;
       e.q = m->q; e.pages_layer = pages_l; e.page_elems = kv->page_elems(); e.page_table = kv->page_table;
@@ -662,7 +718,9 @@ static laser_status verify_impl(laser_model* m, laser_kv* kv, const int32_t* seq
     if (kv_alone) break;
     {
       ProfScope ps(m, 1, stream);
-      if (use_tma_attn && start && !m->precise) {
+      if (q4) {
+        LASER_TRY(attention_int4_launch(m, kv, l, seq_ids, parents, B, Rs, stream));
+      } else if (use_tma_attn && start && !m->precise) {
         LASER_TRY(attention_prefill_launch(m, kv, l, seq_ids, B, stream));
       } else if (use_tma_attn) {
         LASER_TRY(attention_tma_launch(m, kv, l, seq_ids, B, Rs, tree, start != nullptr, stream));

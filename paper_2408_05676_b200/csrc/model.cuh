@@ -26,6 +26,7 @@ struct laser_model {
   __nv_bfloat16* attn = nullptr;   // [R_cap, dq] attention output
   __nv_bfloat16* act = nullptr;    // [R_cap, f] SwiGLU output
   float* sumsq = nullptr;          // [ceil(d/128)][R_cap] per-tile sums of squares of the residual
+  float* qkv = nullptr;            // [R_cap, dqkv] projections of a layer in fp32: steps over a 4-bit cache only, made with the first such cache
   float* rope = nullptr;           // [R_cap, head_dim/2, 2] cos, sin of each row's position
   int32_t* row_pos = nullptr;      // [R_cap] position of the row, -1 = inactive
   int32_t* row_seq = nullptr;      // [R_cap] cache slot of the row
@@ -161,6 +162,18 @@ laser_status attention_tma_launch(laser_model* m, laser_kv* kv, int layer, const
                                   cudaStream_t stream);
 // The same for the chunks of a prefill pass (default mode; head_dim 64 or 128 as above).
 laser_status attention_prefill_launch(laser_model* m, laser_kv* kv, int layer, const int32_t* seq_ids, int n_chunks, cudaStream_t stream);
+
+// A layer's part of a forward over a 4-bit cache.  Queries (where wanted) to m->q rotated, keys and values of the rows that the step's
+// tables name to the cache, from fp32 rows of ld elements, q | k | v.
+laser_status append_step_rows(laser_model* m, laser_kv* kv, int layer, const float* qkv, int64_t ld, bool queries, int rows, cudaStream_t stream);
+// Attention of those rows, m->q to m->attn (rows that are not active are left as they are).
+laser_status attention_int4_launch(laser_model* m, laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* parents, int B, int Rs,
+                                   cudaStream_t stream);
+int attention_int4_max_groups();                                  // most sequences or prompt chunks of a launch
+size_t attention_int4_part_floats(int head_dim, int ctas);        // room for its partial results
+laser_status kv_copy_q4(const laser_kv* kv, int seq, int layer, int pos0, int n, void* k, void* v, bool to_pages, cudaStream_t stream);
+laser_status compact_path_q4(laser_kv* kv, const int32_t* seq_ids, const int32_t* path_rows, const int32_t* n_accept, int B, int row_stride,
+                             cudaStream_t stream);
 
 // Prompt processing: the verify forward without the LM head over chunks of up to kPrefillChunk prompt tokens.  Chunk i is
 // n_rows[i] tokens of cache slot seq_ids[i] from position start[i] on; chunks of one prompt may share a call, in any order:
