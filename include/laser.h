@@ -241,7 +241,7 @@ laser_status laser_kv_free(laser_kv* kv);
  * Every call that takes a cache takes either form: laser_verify_step, _tree, laser_verify_accept and
  * laser_generate write and read it, laser_kv_import rounds to it, laser_kv_export gives the bf16
  * numbers that it stands for, and laser_accept_tree / laser_kv_compact_path move codes as they are.
- * Logits are those of a model whose keys and values are rounded this way; 2048 sequences a step at most.
+ * Logits are those of a model whose keys and values are rounded this way; 1024 sequences a step at most.
  * The first such cache of a model also allocates fp32 rows for a layer's projections (a model that did
  * not create the cache does so in its first step over it, which must not be under stream capture).
  * Errors: UNSUPPORTED (head_dim other than 64 and 128, a precise model), INVALID_ARG, OOM. */
@@ -302,7 +302,7 @@ laser_status laser_kv_append(laser_kv* kv, int32_t layer, const int32_t* seq_ids
  *        as they are
  * The work is divided evenly over the SMs whatever the lengths.  It keeps partial results in memory of
  * the cache's.  Asynchronous on `stream`.
- * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 2048); on the device as above,
+ * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 1024, or tiles of rows x pages beyond 2^31 a sequence); on the device as above,
  * and TIMEOUT. */
 laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int32_t* seq_ids, const int32_t* parents,
                                const int32_t* n_rows, int32_t B, int32_t rows, const void* q, int64_t q_stride,

@@ -1,12 +1,12 @@
 // Attention of a step's rows over a 4-bit paged cache (int4.cuh): o = sum_t p_t v_t / sum_t p_t, p_t = exp(q . k_t / sqrt(dh)), where row i
 // sees the sequence's cached tokens and, of the step's own rows, 0 .. i (chain) or its ancestors and itself (token tree).
 //
-// The rows of a sequence that share a kv head (rows x n_heads / n_kv_heads) form tiles of 16 - or of 8, where all of them fit that.
-// (sequence, kv head, tile) is a unit; all units' pages, one after another, are divided evenly over the SMs (one CTA each) and within a
-// CTA over its warps, so ragged lengths leave nobody idle.  A warp walks its pages alone: a page's K and V of a head, codes and scales,
-// are one bulk copy into the warp's own ring of shared-memory stages, and the codes become bf16 pairs in registers in the order of the
-// MMA's fragments.  16 tokens a step: S = Q K^T and O += P V (tiles of 8 rows: the transposes of both, K and V as the 16-row operand,
-// which halves the MMAs), the sum of P as the product with ones.
+// The rows of a sequence that share a kv head (rows x n_heads / n_kv_heads) form tiles of 8 NT rows, NT = 1 .. 5.  (sequence, kv head,
+// tile) is a unit; all units' pages, one after another, are divided evenly over the SMs (one CTA each) and within a CTA over its warps, so
+// ragged lengths leave nobody idle.  A warp walks its pages alone: a page's K and V of a head, codes and scales, are one bulk copy into
+// the warp's own ring of shared-memory stages, and the codes become bf16 pairs in registers in the order of the MMA's fragments.  16
+// tokens a step, S^T = K Q^T and O^T += V^T P^T: tokens and features are the 16-row operand, so that what was unpacked serves all of the
+// tile's rows, eight at a time, and few rows waste little.  The sum of P is the product with ones.
 //
 // The softmax's reference m is a whole number in the exponent of two: raising it multiplies p and O by powers of two, exactly, so a
 // row's result does not depend on where its walk was cut but for the order of fp32 sums.  It is raised only when a score exceeds it by
@@ -28,20 +28,29 @@ namespace laser {
 namespace {
 
 using bf16 = __nv_bfloat16;
-constexpr int kMaxSeqs = 2048;     // sequences (or prompt chunks) of a call: their offsets are in shared memory
+constexpr int kMaxSeqs = 1024;     // sequences (or prompt chunks) of a call: their offsets are in shared memory
 constexpr int kMinPages = 2;       // least pages of a warp: two are in flight together anyway
+constexpr int kMostTiles = 5;      // of eight rows in a tile: O takes 160 registers then
 
-template <int DH, bool M8>
+template <int DH, int NT>
 struct Sizes {
-  static constexpr int kWarps = M8 ? 16 : 12;            // 128 or 168 registers a thread
-  static constexpr int kStages = DH == 128 ? 4 : 8;
-  static constexpr int kRows = M8 ? 8 : 16;
-  static constexpr int kBlock = 20 * DH;                 // bytes of a page and head
-  static constexpr int kRegs = M8 ? DH / 4 : DH / 2;     // O registers of a lane
-  static constexpr int kRecord = (kRegs + 4) * 32;       // floats of a piece: O, m, sums
-  static constexpr int kSlice = M8 ? 4 : 8;              // registers that are merged together: neighbouring features
-  static constexpr int kSlices = kRegs / kSlice;
-  static constexpr int smem(int B) { return kWarps * kStages * (kBlock + 8) + (B + 1) * 16; }
+  static constexpr int kRegsO = NT * DH / 4;             // O registers of a lane
+  // as many warps as the registers allow without spills
+  static constexpr int kWarps = kRegsO <= 32 ? 16 : kRegsO <= 64 ? 12 : 8;
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kBlock = q4_block_bytes(DH);      // bytes of a page and head
+  static constexpr int kStages = DH == 64 ? 6 : 4;
+  static constexpr bool kQInSmem = NT > 1;               // each lane's share of Q is put by and read again for every page
+  static constexpr int kQBytes = kQInSmem ? NT * DH / 8 * 4 * 32 : 0;
+  static constexpr int kSlices = NT * DH / 16;           // of O: four registers, two neighbouring features of two rows
+  static constexpr int kOBytes = kSlices * 512;          // O of a piece
+  // A warp's memory: its ring and Q; when those are done with, O of the piece that it ends with and slices of others' first pieces
+  static constexpr int kLoop = kStages * kBlock + kQBytes;
+  static constexpr int kRegion = kLoop > kOBytes ? kLoop : kOBytes;
+  static constexpr int kFetched = (kRegion - kOBytes) / 512;
+  static constexpr int kRecord = kOBytes / 4 + 16 * NT;  // floats of a CTA's piece: O, then (m, sum) of the rows
+  static constexpr int smem(int B) { return kWarps * (kRegion + kStages * 8) + (B + 1) * 8 + B * 12; }
+  static size_t part_floats(int ctas) { return size_t(ctas) * (kWarps * (kOBytes / 4) + 2 * kRecord); }
 };
 
 struct AttnArgs {
@@ -54,6 +63,8 @@ struct AttnArgs {
   const bf16* q;
   bf16* out;
   long long ldq, ldo;                          // elements between rows
+  int vec_out;                                 // rows of out are 16-byte aligned
+  unsigned group_inv;                          // 2^32 / G rounded up (G > 1)
   float scale;                                 // log2(e) / sqrt(dh)
   float *part;
   int32_t *arrived, *status;
@@ -69,8 +80,13 @@ __device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
 }
-// two codes at bits 3 .. 6 of the halves -> the two values
-__device__ __forceinline__ uint32_t values(uint32_t w, uint32_t s2, uint32_t z2) { return fma2((w & 0x00780078u) | 0x41804180u, s2, z2); }
+// two codes at bits 3 .. 6 of the halves -> the two values.  (w & 0x00780078) | 0x41804180 as one instruction: of two constants the
+// compiler makes two, and the kernel's busiest pipe is the one for logic and shifts.
+__device__ __forceinline__ uint32_t values(uint32_t w, uint32_t s2, uint32_t z2) {
+  uint32_t u;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(u) : "r"(w), "r"(0x00780078u), "r"(0x41804180u));
+  return fma2(u, s2, z2);
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
@@ -80,6 +96,10 @@ __device__ __forceinline__ void copy_block(uint32_t dst, const void* src, int by
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void lds(uint32_t (&w)[N], const uint8_t* p) {
   if (N == 4) {
@@ -91,22 +111,37 @@ __device__ __forceinline__ void lds(uint32_t (&w)[N], const uint8_t* p) {
   }
 }
 
-template <int DH, bool M8>
-__global__ void __launch_bounds__(Sizes<DH, M8>::kWarps * 32, 1)
+// a unit: its sequence, kv head and first row; its first page (from the CTA's first) and its pages
+struct Segment { int b, hk, row0, start, pages; };
+// one that is cut: the warps whose pieces are this CTA's; whether the last of them went on behind it; whether other CTAs have pieces, and
+// then whether they have its beginning
+struct Cut { Segment seg; int first, last; bool early, open, begun; };
+constexpr float kNothing = 1e30f;      // -m of rows that have seen nothing
+
+template <int DH, int NT>
+__global__ void __launch_bounds__(Sizes<DH, NT>::kWarps * 32, 1)
 attn_int4_kernel(const AttnArgs a) {
-  using Z = Sizes<DH, M8>;
+  using Z = Sizes<DH, NT>;
   constexpr int W = Z::kWarps, ST = Z::kStages, TM = Z::kRows, BLK = Z::kBlock;
   constexpr int KW = DH / 32;            // words of a lane's K (of a token) or V (of two tokens)
-  constexpr int CPG = DH / 8;            // output features of a lane's column
+  constexpr int CPG = DH / 8;            // output features of a lane
+  constexpr int MT = DH / 16;            // 16-feature tiles
+  constexpr int QC = DH / 32;            // 16-byte pieces of a lane's share of a Q row
   extern __shared__ __align__(128) uint8_t smem[];
-  uint8_t* const ring = smem;                                                       // [W][ST][BLK]
-  uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + W * ST * BLK);          // [W][ST]
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + W * Z::kRegion);        // [W][ST], behind the warps' regions
   long long* const s_pre = reinterpret_cast<long long*>(bars + W * ST);             // [B + 1] pages before a sequence
   int* const s_ctx = reinterpret_cast<int*>(s_pre + a.B + 1);                       // [B]
   int* const s_nr = s_ctx + a.B;                                                    // [B]
+  int* const s_seq = s_nr + a.B;                                                    // [B]
   __shared__ long long s_sum[W];
-  __shared__ int s_abort, s_last[2];
+  __shared__ unsigned long long s_path[W][64];      // token trees: the rows that a row of the warp's sequence sees
+  __shared__ Segment s_seg[W][2];                   // the units of a warp's first and of its last page
+  __shared__ Cut s_cut[2 * W];
+  __shared__ float2 s_ml[W][2][TM];                 // m and sum of the rows of the piece that a warp began with, if it went on; that it ended with
+  __shared__ int s_abort, s_cuts, s_last[2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3;
+  // a row is verify row row / G, head row % G of its kv head
+  auto verify_row = [&](int row) { return a.G == 1 ? row : int(__umulhi(unsigned(row), a.group_inv)); };
 
   next_may_launch();
   if (tid == 0) s_abort = 0;
@@ -119,15 +154,15 @@ attn_int4_kernel(const AttnArgs a) {
 
   // ---- the units: pages of all sequences, one after another ----
   auto tiles_of = [&](int nr) { return (nr * a.G + TM - 1) / TM; };
-  long long carry = 0;
+  long long total = 0;
   for (int b0 = 0; b0 < a.B; b0 += W * 32) {
     const int b = b0 + tid;
-    int ctx = 0, nr = 0;
+    int ctx = 0, nr = 0, seq = 0;
     if (b < a.B) {
+      seq = a.seq_ids[b];
       if (a.row_ctx) {
         ctx = a.row_ctx[b]; nr = a.row_n[b];
       } else {
-        const int seq = a.seq_ids[b];
         nr = min(max(a.n_rows[b], 0), a.Rs);
         if (seq < 0 || seq >= a.max_seqs) {
           if (nr > 0 && blockIdx.x == 0) atomicCAS(a.status, 0, LASER_ERR_INVALID_ARG);
@@ -140,9 +175,9 @@ attn_int4_kernel(const AttnArgs a) {
           }
         }
       }
-      s_ctx[b] = ctx; s_nr[b] = nr;
+      s_ctx[b] = ctx; s_nr[b] = nr; s_seq[b] = seq;
     }
-    const long long mine = nr > 0 ? (long long)a.Hkv * tiles_of(nr) * ((ctx + nr + 15) >> 4) : 0;
+    const long long mine = nr > 0 ? (long long)(a.Hkv * tiles_of(nr)) * ((ctx + nr + 15) >> 4) : 0;
     long long x = mine;
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, x, o);
@@ -150,114 +185,142 @@ attn_int4_kernel(const AttnArgs a) {
     }
     if (lane == 31) s_sum[warp] = x;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) x += s_sum[w];
-    if (b < a.B) s_pre[b] = carry + x - mine;
-    for (int w = 0; w < W; ++w) carry += s_sum[w];
+    long long all = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (w == warp) x += all;
+      all += s_sum[w];
+    }
+    if (b < a.B) s_pre[b] = total + x - mine;
+    total += all;
     __syncthreads();
   }
-  if (tid == 0) s_pre[a.B] = carry;
-  __syncthreads();
   if (a.row_ctx) wait_for_earlier();
-  const long long total = carry;
-  const long long per_cta = max((total + gridDim.x - 1) / gridDim.x, (long long)(2 * kMinPages));
-  const long long c0 = per_cta * blockIdx.x, c1 = min(total, c0 + per_cta);
-  if (c0 >= c1) return;
-  const int per_warp = max(int((per_cta + W - 1) / W), kMinPages);
-  const long long w0 = c0 + (long long)per_warp * warp;
-  const int n = int(max(min(c1 - w0, (long long)per_warp), 0ll));     // this warp's pages
+  // (a CTA's share is below 2^31 pages: the cache has no more than that, and a call no more tiles than that allows)
+  const int per_cta = max(total <= 0xffffffffll ? int((unsigned(total) + gridDim.x - 1) / gridDim.x) : int((total + gridDim.x - 1) / gridDim.x), 2 * kMinPages);
+  const long long c0 = (long long)per_cta * blockIdx.x;
+  if (c0 >= total) return;
+  const int span = int(min(total - c0, (long long)per_cta));      // this CTA's pages
+  const int per_warp = max((per_cta + W - 1) / W, kMinPages);
+  const int n = min(span - per_warp * warp, per_warp);            // this warp's (none, if that is negative)
 
-  struct Unit { int b, pages; long long at; };     // a sequence, pages of each of its units, offset of a place in it
-  auto find = [&](long long x) {                    // the sequence that page x belongs to
-    int lo = 0, hi = a.B - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_pre[mid] <= x) lo = mid; else hi = mid - 1;
-    }
-    return Unit{lo, (s_ctx[lo] + s_nr[lo] + 15) >> 4, x - s_pre[lo]};
-  };
-  float* const part = a.part + size_t(blockIdx.x) * (2 * W) * Z::kRecord;                       // the warps' pieces
-  float* const cta_part = a.part + (size_t(gridDim.x) * (2 * W) + 2 * blockIdx.x) * Z::kRecord;  // this CTA's
-
-  // a feature pair of a row: the output's place, and its two values
-  auto store2 = [&](int b, int hk, int row, int nrows, int feature, float x, float y) {
-    if (row < nrows) {
-      const int i = row / a.G, j = row % a.G;
-      *reinterpret_cast<uint32_t*>(a.out + (size_t(b) * a.Rs + i) * a.ldo + size_t(hk * a.G + j) * DH + feature) = pack_bf16(x, y);
-    }
-  };
+  float* const all_part = a.part + size_t(gridDim.x) * W * (Z::kOBytes / 4);                   // [CTA][2] records: CTAs' pieces
+  float4* const my_part = reinterpret_cast<float4*>(a.part) + size_t(blockIdx.x * W + warp) * (Z::kSlices * 32) + lane;   // the warp's first piece
 
   if (n > 0) {
-    uint8_t* const my_ring = ring + warp * ST * BLK;
+    uint8_t* const my_ring = smem + warp * Z::kRegion;
     const uint32_t ring_at = smem_u32(my_ring), bar_at = smem_u32(bars + warp * ST);
-    // ---- copies: a cursor that runs ST pages ahead; 32 page numbers are held, one a lane ----
-    Unit u = find(w0);
-    int p_b = u.b, p_pages = u.pages, p_unit = int(u.at / u.pages), p_page = int(u.at % u.pages), p_base = -1, p_ids = 0;
-    int p_units = a.Hkv * tiles_of(s_nr[p_b]), p_tiles = tiles_of(s_nr[p_b]);
-    auto request = [&](int it) {
-      if (p_base < 0 || p_page < p_base || p_page >= p_base + 32) {
-        p_base = p_page & ~31;
-        p_ids = a.page_table[size_t(a.seq_ids[p_b]) * a.pages_per_seq + min(p_base + lane, p_pages - 1)];
+    // ---- where the warp begins ----
+    int b, tile, hk, page;
+    {
+      const long long x = c0 + per_warp * warp;
+      int lo = 0, hi = a.B - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_pre[mid] <= x) lo = mid; else hi = mid - 1;
       }
-      const int phys = __shfl_sync(0xffffffffu, p_ids, p_page - p_base);
-      if (lane == 0) {
-        const int s = it % ST;
+      b = lo;
+      const unsigned at = unsigned(x - s_pre[b]), pg = unsigned(s_ctx[b] + s_nr[b] + 15) >> 4, unit = at / pg, tl = unsigned(tiles_of(s_nr[b]));
+      page = int(at - unit * pg); hk = int(unit / tl); tile = int(unit - hk * tl);
+    }
+    int pages = (s_ctx[b] + s_nr[b] + 15) >> 4, tiles = tiles_of(s_nr[b]);
+
+    // ---- copies: a cursor that runs ST pages ahead; of 32 pages each lane holds one's address and requests that page ----
+    int p_b = b, p_tile = tile, p_hk = hk, p_page = page, p_pages = pages, p_tiles = tiles, p_window = -1, p_id = 0;
+    const uint8_t* p_src = nullptr;
+    auto aim = [&]() {
+      if (p_window != (p_page & ~31)) {
+        p_window = p_page & ~31;
+        p_id = a.page_table[size_t(s_seq[p_b]) * a.pages_per_seq + min(p_window + lane, p_pages - 1)];
+      }
+      p_src = a.pages + (size_t(p_id) * a.Hkv + p_hk) * BLK;
+    };
+    auto request = [&](int s) {
+      if (lane == (p_page & 31)) {
         mbar_expect_tx(bar_at + s * 8, BLK);
-        copy_block(ring_at + s * BLK, a.pages + (size_t(phys) * a.Hkv + p_unit / p_tiles) * BLK, BLK, bar_at + s * 8);
+        copy_block(ring_at + s * BLK, p_src, BLK, bar_at + s * 8);
       }
       if (++p_page == p_pages) {
         p_page = 0;
-        if (++p_unit == p_units) {
-          p_unit = 0; p_base = -1;
-          do { ++p_b; } while (p_b < a.B && s_nr[p_b] == 0);
-          if (p_b < a.B) {
+        if (++p_tile == p_tiles) {
+          p_tile = 0;
+          if (++p_hk == a.Hkv) {
+            p_hk = 0;
+            do { ++p_b; } while (p_b < a.B && s_nr[p_b] == 0);
+            if (p_b >= a.B) return;             // (the last page of all: nothing is requested after it)
+            p_window = -1;
             p_pages = (s_ctx[p_b] + s_nr[p_b] + 15) >> 4;
             p_tiles = tiles_of(s_nr[p_b]);
-            p_units = a.Hkv * p_tiles;
           }
         }
+        aim();
+      } else if ((p_page & 31) == 0) {
+        aim();
       }
     };
     __syncwarp();
-    for (int it = 0; it < min(n, ST); ++it) request(it);
+    aim();
+#pragma unroll 1
+    for (int s = 0; s < min(n, ST); ++s) request(s);
 
-    int it = 0, b = u.b, pages = u.pages, tiles = tiles_of(s_nr[b]), unit = int(u.at / u.pages), page = int(u.at % u.pages);
+    int it = 0, path_b = -1, stage = 0;
+    uint32_t parity = 0;
     bool ok = true;
     while (it < n && ok) {
       // ---- a unit, or what of it is this warp's ----
-      const int hk = unit / tiles, row0 = (unit % tiles) * TM, nr = s_nr[b], ctx = s_ctx[b], nrows = nr * a.G;
+      const int row0 = tile * TM, nr = s_nr[b], ctx = s_ctx[b], nrows = nr * a.G;
       const int first = page, last = min(pages, page + (n - it));
+      if (lane == 0) {
+        const Segment seg{b, hk, row0, per_warp * warp + it - page, pages};
+        if (it == 0) s_seg[warp][0] = seg;
+        if (n - it <= pages - page) s_seg[warp][1] = seg;
+      }
       // Q: a lane's features are those of its K words
-      uint32_t qa[M8 ? 1 : 2][DH / 8];
+      uint32_t qa[Z::kQInSmem ? 1 : NT][DH / 8];
+      uint4* const my_q = reinterpret_cast<uint4*>(my_ring + ST * BLK) + lane;
 #pragma unroll
-      for (int y = 0; y < (M8 ? 1 : 2); ++y) {
-        const int row = row0 + g + 8 * y, i = row / a.G, j = row % a.G;
+      for (int t = 0; t < NT; ++t) {
+        const int row = row0 + 8 * t + g, i = verify_row(row), j = row - i * a.G;
         const bf16* src = a.q + (size_t(b) * a.Rs + i) * a.ldq + size_t(hk * a.G + j) * DH + qd * (DH / 4);
 #pragma unroll
-        for (int x = 0; x < DH / 32; ++x) {
+        for (int x = 0; x < QC; ++x) {
           const uint4 v = row < nrows ? reinterpret_cast<const uint4*>(src)[x] : make_uint4(0, 0, 0, 0);
-          qa[y][4 * x] = v.x; qa[y][4 * x + 1] = v.y; qa[y][4 * x + 2] = v.z; qa[y][4 * x + 3] = v.w;
+          if (Z::kQInSmem) {
+            my_q[(t * QC + x) * 32] = v;
+          } else {
+            uint32_t* to = qa[Z::kQInSmem ? 0 : t] + 4 * x;
+            to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
+          }
         }
       }
-      // what the lane's two rows (M8: columns 2 qd, 2 qd + 1) see of the step's own rows: bit j = row j; chains by their last key
-      const int ra = min(row0 + (M8 ? 2 * qd : g), nrows - 1) / a.G, rb = min(row0 + (M8 ? 2 * qd + 1 : g + 8), nrows - 1) / a.G;
-      unsigned long long see0 = 0, see1 = 0;
-      if (a.parents) {
+      if (a.parents && path_b != b) {
         unsigned long long mask[2];
         tree_paths(a.parents + size_t(b) * a.Rs, nr, lane, mask);
-        see0 = tree_path_of(mask, ra);
-        see1 = tree_path_of(mask, rb);
+        __syncwarp();
+        s_path[warp][lane] = mask[0];
+        s_path[warp][lane + 32] = mask[1];
+        __syncwarp();
+        path_b = b;
       }
-      float o[Z::kRegs / 4][4], sums[4] = {0.f, 0.f, 0.f, 0.f}, m[2] = {-INFINITY, -INFINITY};
+      // shift = -m, with m the softmax's reference: p = 2^(score x scale + shift)
+      float o[NT][MT][4], sums[NT][4], shift[NT][2];
 #pragma unroll
-      for (int t = 0; t < Z::kRegs / 4; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
+      for (int t = 0; t < NT; ++t) {
+        shift[t][0] = shift[t][1] = kNothing;
+        sums[t][0] = sums[t][1] = sums[t][2] = sums[t][3] = 0.f;
+#pragma unroll
+        for (int f = 0; f < MT; ++f) o[t][f][0] = o[t][f][1] = o[t][f][2] = o[t][f][3] = 0.f;
+      }
 
+#pragma unroll 1
       for (; page < last; ++page, ++it) {
-        const int s = it % ST;
-        if (!mbar_wait_warp(bar_at + s * 8, (it / ST) & 1, &s_abort)) { ok = false; break; }
-        const uint8_t* blk = my_ring + s * BLK;
-        // ---- scores: M16 sc[0], sc[1] = tokens 0 .. 7, 8 .. 15; M8 sc[0] = even, sc[1] = odd steps of the features ----
-        float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        if (!mbar_wait_warp(bar_at + stage * 8, parity, &s_abort)) { ok = false; break; }
+        const uint8_t* blk = my_ring + stage * BLK;
+        // ---- scores: of tokens g and g + 8 (the halves of x) and the lane's rows 2 qd, 2 qd + 1 of each tile ----
+        float x[NT][4];
         {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.f;
           uint32_t k0[KW], k1[KW];
           lds<KW>(k0, blk + q4_k_codes(DH, g, qd * KW));
           lds<KW>(k1, blk + q4_k_codes(DH, g + 8, qd * KW));
@@ -266,73 +329,72 @@ attn_int4_kernel(const AttnArgs a) {
           const uint32_t s0 = __byte_perm(sz0, 0, 0x1010), z0 = __byte_perm(sz0, 0, 0x3232);
           const uint32_t s1 = __byte_perm(sz1, 0, 0x1010), z1 = __byte_perm(sz1, 0, 0x3232);
 #pragma unroll
-          for (int w = 0; w < KW; ++w)
+          for (int w = 0; w < KW; ++w) {
+            const uint32_t ka[4] = {values(k0[w], s0, z0), values(k1[w], s1, z1), values(__funnelshift_r(k0[w], k0[w], 4), s0, z0),
+                                    values(__funnelshift_r(k1[w], k1[w], 4), s1, z1)};
+            const uint32_t kb[4] = {values(__funnelshift_r(k0[w], k0[w], 8), s0, z0), values(__funnelshift_r(k1[w], k1[w], 8), s1, z1),
+                                    values(__funnelshift_r(k0[w], k0[w], 12), s0, z0), values(__funnelshift_r(k1[w], k1[w], 12), s1, z1)};
+            uint4 q[NT];
 #pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-              const uint32_t x0 = values(e ? __funnelshift_r(k0[w], k0[w], 8) : k0[w], s0, z0), x1 = values(__funnelshift_r(k0[w], k0[w], 4 * e + 4), s0, z0);
-              const uint32_t y0 = values(e ? __funnelshift_r(k1[w], k1[w], 8) : k1[w], s1, z1), y1 = values(__funnelshift_r(k1[w], k1[w], 4 * e + 4), s1, z1);
-              const int r = 4 * w + e;
-              if (M8) {
-                const uint32_t ka[4] = {x0, y0, x1, y1};
-                mma16816(sc[e / 2], ka, qa[0][r], qa[0][r + 1]);
+            for (int t = 0; t < NT; ++t) {
+              const uint32_t* own = qa[Z::kQInSmem ? 0 : t] + 4 * w;
+              q[t] = Z::kQInSmem ? my_q[(t * QC + w) * 32] : make_uint4(own[0], own[1], own[2], own[3]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816(x[t], ka, q[t].x, q[t].y);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816(x[t], kb, q[t].z, q[t].w);
+          }
+        }
+        if (page * 16 + 15 >= ctx) {      // some of the step's own rows, or slots behind them
+          const int rel0 = page * 16 + g - ctx, rel1 = rel0 + 8;
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const int i = verify_row(min(row0 + 8 * t + 2 * qd + y, nrows - 1));      // (rows that are not active: as the last)
+              if (a.parents) {
+                const unsigned long long see = s_path[warp][i];
+                if (rel0 >= 0 && (rel0 >= 64 || !(see >> (rel0 & 63) & 1))) x[t][y] = -INFINITY;
+                if (rel1 >= 0 && (rel1 >= 64 || !(see >> (rel1 & 63) & 1))) x[t][2 + y] = -INFINITY;
               } else {
-                const uint32_t qf[4] = {qa[0][r], qa[M8 ? 0 : 1][r], qa[0][r + 1], qa[M8 ? 0 : 1][r + 1]};
-                mma16816(sc[0], qf, x0, x1);
-                mma16816(sc[1], qf, y0, y1);
+                if (rel0 > i) x[t][y] = -INFINITY;
+                if (rel1 > i) x[t][2 + y] = -INFINITY;
               }
             }
         }
-        float x[2][4];      // [lane's row][its four tokens], in units of log2
-        if (M8) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) sc[0][c] += sc[1][c];
-        }
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) x[y][c] = M8 ? (c < 2 ? sc[0][2 * c + y] : -INFINITY) : sc[c >> 1][2 * y + (c & 1)];
-        if (page * 16 + 15 >= ctx) {      // some of the step's own rows, or slots behind them
-#pragma unroll
-          for (int c = 0; c < (M8 ? 2 : 4); ++c) {
-            const int rel = page * 16 + (M8 ? g + 8 * c : (c >> 1) * 8 + 2 * qd + (c & 1)) - ctx;
-            if (rel < 0) continue;
-            const bool on0 = a.parents ? rel < 64 && (see0 >> (rel & 63) & 1) : rel <= ra;
-            const bool on1 = a.parents ? rel < 64 && (see1 >> (rel & 63) & 1) : rel <= rb;
-            if (!on0) x[0][c] = -INFINITY;
-            if (!on1) x[1][c] = -INFINITY;
-          }
-        }
-        float top[2];
         bool above = false;
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          top[y] = M8 ? fmaxf(x[y][0], x[y][1]) : fmaxf(fmaxf(x[y][0], x[y][1]), fmaxf(x[y][2], x[y][3]));
-          above = above || top[y] * a.scale > m[y] + 6.f;
-        }
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) above = above || fmaf(fmaxf(x[t][y], x[t][2 + y]), a.scale, shift[t][y]) > 6.f;
         if (__any_sync(0xffffffffu, above)) {
-          float down[2];
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float t = top[y];
+          for (int t = 0; t < NT; ++t) {
+            float down[2];
 #pragma unroll
-            for (int d = M8 ? 4 : 1; d <= (M8 ? 16 : 2); d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-            const float next = fmaxf(m[y], ceilf(t * a.scale));
-            down[y] = m[y] == next ? 1.f : ex2(m[y] - next);
-            m[y] = next;
+            for (int y = 0; y < 2; ++y) {
+              float top = fmaxf(x[t][y], x[t][2 + y]);
+#pragma unroll
+              for (int d = 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              const float next = fminf(shift[t][y], -ceilf(top * a.scale));
+              down[y] = ex2(next - shift[t][y]);
+              shift[t][y] = next;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sums[t][c] *= down[c & 1];
+#pragma unroll
+            for (int f = 0; f < MT; ++f)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) o[t][f][c] *= down[c & 1];
           }
-#pragma unroll
-          for (int t = 0; t < Z::kRegs / 4; ++t)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) o[t][c] *= down[M8 ? c & 1 : c >> 1];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) sums[c] *= down[M8 ? c & 1 : c >> 1];
         }
-        float p[2][4];
+        // ---- probabilities: from (token, row) to the second product's fragments, a row's tokens 2 qd, 2 qd + 1 (and 8 on) in lane g ----
+        uint32_t p0[NT], p1[NT];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const float mu = m[y] == -INFINITY ? 0.f : m[y];
-#pragma unroll
-          for (int c = 0; c < (M8 ? 2 : 4); ++c) p[y][c] = ex2(fmaf(x[y][c], a.scale, -mu));
+        for (int t = 0; t < NT; ++t) {
+          p0[t] = transpose8(pack_bf16(ex2(fmaf(x[t][0], a.scale, shift[t][0])), ex2(fmaf(x[t][1], a.scale, shift[t][1]))));
+          p1[t] = transpose8(pack_bf16(ex2(fmaf(x[t][2], a.scale, shift[t][0])), ex2(fmaf(x[t][3], a.scale, shift[t][1]))));
         }
         // ---- values ----
         {
@@ -340,84 +402,84 @@ attn_int4_kernel(const AttnArgs a) {
           lds<KW>(v0, blk + 10 * DH + lane * KW * 4);
           lds<KW>(v1, blk + 10 * DH + (32 + lane) * KW * 4);
           lds<4>(sz, blk + 18 * DH + (g * CPG / 32 * 4 + qd) * 16);
-          uint32_t pf[4];
-          if (M8) {
-            pf[0] = transpose8(pack_bf16(p[0][0], p[1][0]));      // tokens g x rows 2 qd .. -> row g, tokens 2 qd ..
-            pf[1] = transpose8(pack_bf16(p[0][1], p[1][1]));
-            const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-            mma16816(sums, ones, pf[0], pf[1]);
-          } else {
-            pf[0] = pack_bf16(p[0][0], p[0][1]);
-            pf[1] = pack_bf16(p[1][0], p[1][1]);
-            pf[2] = pack_bf16(p[0][2], p[0][3]);
-            pf[3] = pack_bf16(p[1][2], p[1][3]);
-            mma16816(sums, pf, 0x3f803f80u, 0x3f803f80u);
-          }
+          const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma16816(sums[t], ones, p0[t], p1[t]);
 #pragma unroll
           for (int w = 0; w < KW; ++w) {
-            const uint32_t e0 = values(v0[w] << 3, sz[0], sz[1]), f0 = values(v1[w] << 3, sz[2], sz[3]);
-            const uint32_t e1 = values(v0[w] >> 1, sz[0], sz[1]), f1 = values(v1[w] >> 1, sz[2], sz[3]);
-            const uint32_t e2 = values(v0[w] >> 5, sz[0], sz[1]), f2 = values(v1[w] >> 5, sz[2], sz[3]);
-            const uint32_t e3 = values(v0[w] >> 9, sz[0], sz[1]), f3 = values(v1[w] >> 9, sz[2], sz[3]);
-            if (M8) {
-              const uint32_t va[4] = {e0, e1, f0, f1}, vb[4] = {e2, e3, f2, f3};
-              mma16816(o[2 * w], va, pf[0], pf[1]);
-              mma16816(o[2 * w + 1], vb, pf[0], pf[1]);
-            } else {
-              mma16816(o[(4 * w) % (Z::kRegs / 4)], pf, e0, f0);
-              mma16816(o[(4 * w + 1) % (Z::kRegs / 4)], pf, e1, f1);
-              mma16816(o[(4 * w + 2) % (Z::kRegs / 4)], pf, e2, f2);
-              mma16816(o[(4 * w + 3) % (Z::kRegs / 4)], pf, e3, f3);
-            }
+            const uint32_t va[4] = {values(v0[w] << 3, sz[0], sz[1]), values(v0[w] >> 1, sz[0], sz[1]), values(v1[w] << 3, sz[2], sz[3]),
+                                    values(v1[w] >> 1, sz[2], sz[3])};
+            const uint32_t vb[4] = {values(v0[w] >> 5, sz[0], sz[1]), values(v0[w] >> 9, sz[0], sz[1]), values(v1[w] >> 5, sz[2], sz[3]),
+                                    values(v1[w] >> 9, sz[2], sz[3])};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816(o[t][2 * w], va, p0[t], p1[t]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816(o[t][2 * w + 1], vb, p0[t], p1[t]);
           }
         }
         __syncwarp();
-        if (it + ST < n) request(it + ST);
+        if (it + ST < n) request(stage);
+        if (++stage == ST) { stage = 0; parity ^= 1; }
       }
       if (!ok) break;
 
       // ---- the unit's result, or the piece that this warp has of it ----
-      const int lane_row0 = row0 + (M8 ? 2 * qd : g), lane_row1 = row0 + (M8 ? 2 * qd + 1 : g + 8);
-      const float l0 = sums[0], l1 = M8 ? sums[1] : sums[2];
       if (first == 0 && last == pages) {
-        const float inv0 = 1.f / l0, inv1 = 1.f / l1;     // (a row sees itself: its sum is not zero)
 #pragma unroll
-        for (int t = 0; t < Z::kRegs / 4; t += M8 ? 1 : 2) {
-          if (M8) {
-            store2(b, hk, lane_row0, nrows, CPG * g + 2 * t, o[t][0] * inv0, o[t][2] * inv0);
-            store2(b, hk, lane_row1, nrows, CPG * g + 2 * t, o[t][1] * inv1, o[t][3] * inv1);
-          } else {
-            const int t1 = (t + 1) % (Z::kRegs / 4);
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              store2(b, hk, lane_row0, nrows, CPG * (2 * qd + c) + t, o[t][c] * inv0, o[t1][c] * inv0);
-              store2(b, hk, lane_row1, nrows, CPG * (2 * qd + c) + t, o[t][2 + c] * inv1, o[t1][2 + c] * inv1);
+          for (int y = 0; y < 2; ++y) {
+            const int row = row0 + 8 * t + 2 * qd + y;
+            if (row >= nrows) continue;
+            const float inv = 1.f / sums[t][y];      // (a row sees itself: its sum is not zero)
+            const int i = verify_row(row), j = row - i * a.G;
+            bf16* dst = a.out + (size_t(b) * a.Rs + i) * a.ldo + size_t(hk * a.G + j) * DH + CPG * g;
+            uint32_t w[MT];
+#pragma unroll
+            for (int f = 0; f < MT; ++f) w[f] = pack_bf16(o[t][f][y] * inv, o[t][f][2 + y] * inv);
+            if (a.vec_out) {
+#pragma unroll
+              for (int f = 0; f < MT; f += 4) *reinterpret_cast<uint4*>(dst + 2 * f) = make_uint4(w[f], w[f + 1], w[f + 2], w[f + 3]);
+            } else {
+#pragma unroll
+              for (int f = 0; f < MT; ++f) *reinterpret_cast<uint32_t*>(dst + 2 * f) = w[f];
             }
           }
-        }
       } else {
-        float* rec = part + (2 * warp + (first == 0 ? 1 : 0)) * Z::kRecord + lane;
+        const bool early = it < n;      // the warp goes on: its memory is not free yet
+        __syncwarp();
 #pragma unroll
-        for (int t = 0; t < Z::kRegs / 4; ++t)
+        for (int t = 0; t < NT; ++t) {
+          if (row0 + 8 * t >= nrows) break;      // (no row of the tile)
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if ((M8 ? c & 1 : c >> 1) ? lane_row1 < nrows : lane_row0 < nrows) __stcg(rec + (4 * t + c) * 32, o[t][c]);
-        __stcg(rec + Z::kRegs * 32, m[0]);
-        __stcg(rec + (Z::kRegs + 1) * 32, m[1]);
-        __stcg(rec + (Z::kRegs + 2) * 32, l0);
-        __stcg(rec + (Z::kRegs + 3) * 32, l1);
+          for (int f = 0; f < MT; ++f) {
+            const float4 v = make_float4(o[t][f][0], o[t][f][1], o[t][f][2], o[t][f][3]);
+            if (early) __stcg(my_part + (t * MT + f) * 32, v);
+            else reinterpret_cast<float4*>(my_ring)[(t * MT + f) * 32 + lane] = v;
+          }
+          if (g == 0) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) s_ml[warp][early ? 0 : 1][8 * t + 2 * qd + y] = make_float2(shift[t][y] == kNothing ? -INFINITY : -shift[t][y], sums[t][y]);
+          }
+        }
       }
       if (page == pages) {
         page = 0;
-        if (++unit == a.Hkv * tiles) {
-          unit = 0;
-          do { ++b; } while (b < a.B && s_nr[b] == 0);
-          if (b < a.B) { pages = (s_ctx[b] + s_nr[b] + 15) >> 4; tiles = tiles_of(s_nr[b]); }
+        if (++tile == tiles) {
+          tile = 0;
+          if (++hk == a.Hkv) {
+            hk = 0;
+            do { ++b; } while (b < a.B && s_nr[b] == 0);
+            if (b < a.B) { pages = (s_ctx[b] + s_nr[b] + 15) >> 4; tiles = tiles_of(s_nr[b]); }
+          }
         }
       }
     }
     if (!ok && lane == 0)     // copies in flight land before the CTA's memory goes
-      for (int x = it; x < min(n, it + ST); ++x) mbar_drain(bar_at + (x % ST) * 8, (x / ST) & 1);
+      for (int x = it; x < min(n, it + ST); ++x) {
+        mbar_drain(bar_at + stage * 8, parity);
+        if (++stage == ST) { stage = 0; parity ^= 1; }
+      }
   }
   __syncthreads();
   if (s_abort) {
@@ -425,105 +487,184 @@ attn_int4_kernel(const AttnArgs a) {
     return;
   }
 
-  // ---- pieces: a warp takes slices of the registers, all pieces of them in order ----
-  // records first, first + stride, .. (the first one at `first`) -> the output, or a record
-  auto merge = [&](const float* head, const float* rest, int count, size_t stride, const Unit& at, float* to) {
-    const int nr = s_nr[at.b], tiles = tiles_of(nr), unit = int(at.at / at.pages), hk = unit / tiles, row0 = (unit % tiles) * TM, nrows = nr * a.G;
-    const int lane_row0 = row0 + (M8 ? 2 * qd : g), lane_row1 = row0 + (M8 ? 2 * qd + 1 : g + 8);
-    for (int sl = warp; sl < Z::kSlices; sl += W) {
-      float acc[Z::kSlice], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < Z::kSlice; ++c) acc[c] = 0.f;
-#pragma unroll 4
-      for (int r = 0; r < count; ++r) {
-        const float* rec = (r == 0 ? head : rest + size_t(r - 1) * stride) + lane;
-        float v[Z::kSlice], f[2];
-#pragma unroll
-        for (int c = 0; c < Z::kSlice; ++c) v[c] = __ldcg(rec + (sl * Z::kSlice + c) * 32);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const float rm = __ldcg(rec + (Z::kRegs + y) * 32), rl = __ldcg(rec + (Z::kRegs + 2 + y) * 32);
-          const float next = fmaxf(m[y], rm);
-          const float old = m[y] == next ? 1.f : ex2(m[y] - next);
-          f[y] = rm == next ? 1.f : ex2(rm - next);
-          if (next == -INFINITY) f[y] = 0.f;        // nothing seen yet
-          m[y] = next;
-          l[y] = l[y] * old + (f[y] == 0.f ? 0.f : rl * f[y]);
-#pragma unroll
-          for (int c = 0; c < Z::kSlice; ++c)
-            if ((M8 ? c & 1 : c >> 1 & 1) == y) acc[c] = acc[c] * old + (f[y] == 0.f ? 0.f : v[c] * f[y]);
-        }
-      }
-      if (to) {
-#pragma unroll
-        for (int c = 0; c < Z::kSlice; ++c) __stcg(to + (sl * Z::kSlice + c) * 32 + lane, acc[c]);
-        if (sl == 0) {
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            __stcg(to + (Z::kRegs + y) * 32 + lane, m[y]);
-            __stcg(to + (Z::kRegs + 2 + y) * 32 + lane, l[y]);
-          }
-        }
-      } else {
-        const float inv0 = 1.f / l[0], inv1 = 1.f / l[1];
-        if (M8) {
-          store2(at.b, hk, lane_row0, nrows, CPG * g + 2 * sl, acc[0] * inv0, acc[2] * inv0);
-          store2(at.b, hk, lane_row1, nrows, CPG * g + 2 * sl, acc[1] * inv1, acc[3] * inv1);
-        } else {
-          constexpr int H2 = Z::kSlice / 2;      // (the second of two neighbouring features)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            store2(at.b, hk, lane_row0, nrows, CPG * (2 * qd + c) + 2 * sl, acc[c] * inv0, acc[(H2 + c) % Z::kSlice] * inv0);
-            store2(at.b, hk, lane_row1, nrows, CPG * (2 * qd + c) + 2 * sl, acc[(2 + c) % Z::kSlice] * inv1, acc[(H2 + 2 + c) % Z::kSlice] * inv1);
-          }
-        }
+  // ---- pieces.  Under load a trip to L2 takes 1.5 us, so they stay in shared memory or come there together.  First those of this CTA:
+  // units around its ends and around the places where one warp follows another ----
+  if (warp == 0) {
+    const int w = lane >> 1, begin_w = w * per_warp;
+    Cut c{};
+    bool here = lane < 2 * W && begin_w < span;
+    if (here) {
+      c.seg = s_seg[w][lane & 1];
+      const int end = c.seg.start + c.seg.pages;
+      here = lane == 0 || s_seg[(lane - 1) >> 1][(lane - 1) & 1].start != c.seg.start;        // (the first to list it)
+      c.first = w;
+      c.last = (min(end, span) - 1) / per_warp;
+      c.begun = c.seg.start < 0;
+      c.open = c.begun || end > span;
+      c.early = end < min((c.last + 1) * per_warp, span);
+      here = here && (c.open || c.first != c.last);       // (else one warp had it all)
+    }
+    const unsigned all = __ballot_sync(0xffffffffu, here);
+    if (here) s_cut[__popc(all & ((1u << lane) - 1))] = c;
+    if (lane == 0) s_cuts = __popc(all);
+  }
+  __syncthreads();
+  const int cuts = s_cuts;
+  // a warp's slice x of cut c; a first piece's slices come from L2, the first few of a warp's all at once
+  auto slices = [&](auto&& each) {
+    int turn = 0, fetched = 0;
+#pragma unroll 1
+    for (int c = 0; c < cuts; ++c) {
+      int sl = warp - turn;
+      if (sl < 0) sl += W;
+      turn = (turn + Z::kSlices) % W;
+      const int rows8 = min((s_nr[s_cut[c].seg.b] * a.G - s_cut[c].seg.row0 + 7) / 8, NT);
+#pragma unroll 1
+      for (; sl < rows8 * MT; sl += W) {
+        each(s_cut[c], sl, fetched);
+        fetched += s_cut[c].early;
       }
     }
   };
-  // units with a piece here: those around the CTA's ends and around the places where one warp follows another
-  long long done = c0;       // units up to here are dealt with
-  long long open_at[2] = {-1, -1};
-  for (int w = 0; w * (long long)per_warp < c1 - c0; ++w) {
-    const long long begin = c0 + (long long)per_warp * w, end = min(c1, begin + per_warp);
-    for (int side = 0; side < 2; ++side) {
-      const long long x = side == 0 ? begin : end - 1;      // the warp's first page, and its last
-      if (x < done) continue;
-      const Unit at = find(x);
-      const long long us = x - at.at % at.pages, ue = us + at.pages;
-      const long long p0 = max(us, c0), p1 = min(ue, c1);
-      done = p1;
-      const int f = int((p0 - c0) / per_warp), e = int((p1 - 1 - c0) / per_warp);     // its warps
-      const bool open = us < c0 || ue > c1;
-      if (f == e && !open) continue;              // one warp had it all
-      // a warp's record 0: a piece without the unit's first page
-      const float* head = part + (2 * f + (us >= c0 ? 1 : 0)) * Z::kRecord;
-      const float* rest = part + (2 * (f + 1)) * Z::kRecord;
-      const int which = us < c0 ? 0 : 1;
-      merge(head, rest, e - f + 1, size_t(2) * Z::kRecord, at, open ? cta_part + which * Z::kRecord : nullptr);
-      if (open) open_at[which] = us;
+  const uint32_t fetch_at = smem_u32(smem) + warp * Z::kRegion + Z::kOBytes + lane * 16;
+  slices([&](const Cut& c, int sl, int fetched) {
+    if (c.early && fetched < Z::kFetched)
+      copy16(fetch_at + fetched * 512, reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * W + c.last) * Z::kSlices + sl) * 32 + lane);
+  });
+  copies_done();
+  __syncwarp();
+  slices([&](const Cut& c, int sl, int fetched) {
+    const int t = sl / MT, f = sl % MT;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll 1
+    for (int x = c.first; x <= c.last; ++x) {
+      const bool early = c.early && x == c.last;
+      float4 v;
+      if (!early) v = reinterpret_cast<const float4*>(smem + x * Z::kRegion)[sl * 32 + lane];
+      else if (fetched < Z::kFetched) v = reinterpret_cast<const float4*>(smem + warp * Z::kRegion + Z::kOBytes)[fetched * 32 + lane];
+      else v = __ldcg(reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * W + x) * Z::kSlices + sl) * 32 + lane);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float2 ml = s_ml[x][early ? 0 : 1][8 * t + 2 * qd + y];
+        const float next = fmaxf(m[y], ml.x), zero = next == -INFINITY ? 0.f : next;
+        const float old = ex2(m[y] - zero), now = ex2(ml.x - zero);
+        m[y] = next;
+        l[y] = l[y] * old + ml.y * now;
+        acc[y] = acc[y] * old + (y ? v.y : v.x) * now;
+        acc[2 + y] = acc[2 + y] * old + (y ? v.w : v.z) * now;
+      }
     }
-  }
-  if (open_at[0] < 0 && open_at[1] < 0) return;
-  __syncthreads();
-  if (tid == 0) {
-    __threadfence();
-    for (int k = 0; k < 2; ++k) {
-      s_last[k] = 0;
-      if (open_at[k] < 0) continue;
-      const Unit at = find(open_at[k]);
-      const long long from = open_at[k] / per_cta, to = (open_at[k] + at.pages - 1) / per_cta;     // the unit's CTAs
-      if (atomicAdd(a.arrived + from, 1) == int(to - from)) { s_last[k] = 1; a.arrived[from] = 0; }
+    if (c.open) {
+      float* rec = all_part + size_t(2 * blockIdx.x + (c.begun ? 0 : 1)) * Z::kRecord;
+      __stcg(reinterpret_cast<float4*>(rec) + sl * 32 + lane, make_float4(acc[0], acc[1], acc[2], acc[3]));
+      if (f == 0 && g == 0) __stcg(reinterpret_cast<float4*>(rec + Z::kOBytes / 4) + 4 * t + qd, make_float4(m[0], l[0], m[1], l[1]));
+    } else {
+      const int nrows = s_nr[c.seg.b] * a.G;
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int row = c.seg.row0 + 8 * t + 2 * qd + y;
+        if (row >= nrows) continue;
+        const float inv = 1.f / l[y];
+        const int i = verify_row(row), j = row - i * a.G;
+        *reinterpret_cast<uint32_t*>(a.out + (size_t(c.seg.b) * a.Rs + i) * a.ldo + size_t(c.seg.hk * a.G + j) * DH + CPG * g + 2 * f) =
+            pack_bf16(acc[y] * inv, acc[2 + y] * inv);
+      }
     }
-    __threadfence();
+  });
+  // the cuts of open units: the first, if the unit began before this CTA, and the last, if it goes on behind it
+  const int open0 = cuts > 0 && s_cut[0].open && s_cut[0].begun ? 0 : -1;
+  const int open1 = cuts > 0 && s_cut[cuts - 1].open && !s_cut[cuts - 1].begun ? cuts - 1 : -1;
+  if (open0 < 0 && open1 < 0) return;
+  __syncthreads();
+  // ---- then, of units that other CTAs have pieces of, those whose last CTA this is ----
+  if (tid < 2) {
+    const int open = tid ? open1 : open0;
+    int last = 0;
+    if (open >= 0) {
+      const Segment& seg = s_cut[open].seg;
+      const int before = seg.start < 0 ? (per_cta - 1 - seg.start) / per_cta : 0, after = (seg.start + seg.pages - 1) / per_cta;     // the unit's other CTAs
+      __threadfence();
+      last = atomicAdd(a.arrived + blockIdx.x - before, 1) == before + after;
+      __threadfence();
+      if (last) a.arrived[blockIdx.x - before] = 0;
+    }
+    s_last[tid] = last;
   }
   __syncthreads();
+  constexpr int kPer = (Z::kSlices + W - 1) / W;      // slices of a warp
+#pragma unroll 1
   for (int k = 0; k < 2; ++k) {
     if (!s_last[k]) continue;
-    const Unit at = find(open_at[k]);
-    const long long from = open_at[k] / per_cta, to = (open_at[k] + at.pages - 1) / per_cta;
-    const float* all = a.part + size_t(gridDim.x) * (2 * W) * Z::kRecord;
-    merge(all + (2 * from + 1) * Z::kRecord, all + 2 * (from + 1) * Z::kRecord, int(to - from + 1), size_t(2) * Z::kRecord, at, nullptr);
+    const Segment seg = s_cut[k ? open1 : open0].seg;
+    const int before = seg.start < 0 ? (per_cta - 1 - seg.start) / per_cta : 0, count = before + (seg.start + seg.pages - 1) / per_cta + 1;
+    // the first CTA's second record, then the others' first ones
+    auto record = [&](int r) { return all_part + (2 * size_t(blockIdx.x - before + r) + (r == 0 ? 1 : 0)) * Z::kRecord; };
+    const int row0 = seg.row0, nrows = s_nr[seg.b] * a.G;
+    const int rows8 = min((nrows - row0 + 7) / 8, NT);                        // groups of eight rows that there are
+    float2* const weight = reinterpret_cast<float2*>(smem);                   // [pieces][rows] (m, sum), then (weight, -); behind them O of pieces
+    const int begin = (count * TM * 8 + 127) & ~127, room = (W * Z::kRegion - begin) / Z::kOBytes;
+    float acc[kPer][4];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) acc[x][0] = acc[x][1] = acc[x][2] = acc[x][3] = 0.f;
+#pragma unroll 1
+    for (int r0 = 0; r0 < count; r0 += room) {
+      const int here = min(room, count - r0);
+      __syncthreads();                      // (what was there before has been read)
+#pragma unroll 1
+      for (int r = 0; r < here; ++r) {
+        const float4* src = reinterpret_cast<const float4*>(record(r0 + r));
+#pragma unroll 1
+        for (int x = tid; x < rows8 * MT * 32; x += W * 32) copy16(smem_u32(smem) + begin + r * Z::kOBytes + x * 16, src + x);
+      }
+      if (r0 == 0) {
+#pragma unroll 1
+        for (int x = tid; x < count * TM; x += W * 32)
+          if (x % TM < 8 * rows8) weight[x] = __ldcg(reinterpret_cast<const float2*>(record(x / TM) + Z::kOBytes / 4) + x % TM);
+        __syncthreads();
+#pragma unroll 1
+        for (int row = warp; row < 8 * rows8; row += W) {
+          float top = -INFINITY, sum = 0.f;
+          for (int r = lane; r < count; r += 32) top = fmaxf(top, weight[r * TM + row].x);
+          for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          for (int r = lane; r < count; r += 32) sum += weight[r * TM + row].y * ex2(weight[r * TM + row].x - top);
+          for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+          for (int r = lane; r < count; r += 32) weight[r * TM + row].x = ex2(weight[r * TM + row].x - top) / sum;
+        }
+      }
+      copies_done();
+      __syncthreads();
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) {
+        const int sl = warp + x * W, t = sl / MT;
+        if (t >= rows8 || sl >= Z::kSlices) break;
+        const float4* src = reinterpret_cast<const float4*>(smem + begin) + sl * 32 + lane;
+#pragma unroll 2
+        for (int r = 0; r < here; ++r) {
+          const float4 v = src[r * (Z::kOBytes / 16)];
+          const float w0 = weight[(r0 + r) * TM + 8 * t + 2 * qd].x, w1 = weight[(r0 + r) * TM + 8 * t + 2 * qd + 1].x;
+          acc[x][0] += v.x * w0; acc[x][1] += v.y * w1; acc[x][2] += v.z * w0; acc[x][3] += v.w * w1;
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int sl = warp + x * W, t = sl / MT, c = sl % MT;
+      if (t >= rows8 || sl >= Z::kSlices) break;
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int row = row0 + 8 * t + 2 * qd + y;
+        if (row >= nrows) continue;
+        const int i = verify_row(row), j = row - i * a.G;
+        *reinterpret_cast<uint32_t*>(a.out + (size_t(seg.b) * a.Rs + i) * a.ldo + size_t(seg.hk * a.G + j) * DH + CPG * g + 2 * c) = pack_bf16(acc[x][y], acc[x][2 + y]);
+      }
+    }
   }
+}
+
+// Tiles of the rows that share a kv head: as few as hold 40 rows at most, then as small as that leaves them.
+int row_tiles(int rows) {
+  const int tiles = ceil_div(rows, 8 * kMostTiles);
+  return ceil_div(ceil_div(rows, tiles), 8);
 }
 
 laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t stream) {
@@ -532,19 +673,35 @@ laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t strea
   a.Hkv = kv->n_kv_heads; a.G = kv->n_heads / kv->n_kv_heads;
   a.page_table = kv->page_table; a.pages_per_seq = kv->pages_per_seq;
   a.scale = float(1.4426950408889634 / std::sqrt(double(kv->head_dim)));
+  a.group_inv = unsigned(((uint64_t(1) << 32) + a.G - 1) / a.G);
   a.part = kv->attn_part; a.arrived = kv->attn_arrived;
+  const int64_t rows = int64_t(a.Rs) * a.G;
+  const int nt = row_tiles(int(std::min<int64_t>(rows, 1 << 28)));
+  const int64_t units = a.Hkv * ceil_div(rows, int64_t(8 * nt));          // of a sequence, at most
+  if (units * kv->pages_per_seq > INT32_MAX) {
+    set_error("%lld row tiles a sequence over caches of %d pages are too many for one call", (long long)units, kv->pages_per_seq);
+    return LASER_ERR_CAPACITY;
+  }
+  a.vec_out = (reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo * 2)) % 16 == 0;
   auto launch = [&](auto kernel, auto sizes) -> laser_status {
     using Z = decltype(sizes);
     const int smem = Z::smem(a.B);
-    const int64_t units = int64_t(a.B) * a.Hkv * ceil_div(a.Rs * a.G, Z::kRows);
-    const unsigned grid = unsigned(std::min<int64_t>(kv->attn_ctas, units * kv->pages_per_seq));
+    const unsigned grid = unsigned(std::min<int64_t>(kv->attn_ctas, units * a.B * kv->pages_per_seq));
     LASER_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     LASER_CUDA(launch_overlapped(kernel, dim3(grid), Z::kWarps * 32, size_t(smem), stream, a));
     return LASER_OK;
   };
-  const bool m8 = a.Rs * a.G <= 8;
-  if (kv->head_dim == 128) LASER_TRY(m8 ? launch(attn_int4_kernel<128, true>, Sizes<128, true>{}) : launch(attn_int4_kernel<128, false>, Sizes<128, false>{}));
-  else LASER_TRY(m8 ? launch(attn_int4_kernel<64, true>, Sizes<64, true>{}) : launch(attn_int4_kernel<64, false>, Sizes<64, false>{}));
+  auto by_tiles = [&](auto dh) -> laser_status {
+    constexpr int D = decltype(dh)::value;
+    switch (nt) {
+      case 1: return launch(attn_int4_kernel<D, 1>, Sizes<D, 1>{});
+      case 2: return launch(attn_int4_kernel<D, 2>, Sizes<D, 2>{});
+      case 3: return launch(attn_int4_kernel<D, 3>, Sizes<D, 3>{});
+      case 4: return launch(attn_int4_kernel<D, 4>, Sizes<D, 4>{});
+      default: return launch(attn_int4_kernel<D, 5>, Sizes<D, 5>{});
+    }
+  };
+  LASER_TRY(kv->head_dim == 128 ? by_tiles(std::integral_constant<int, 128>{}) : by_tiles(std::integral_constant<int, 64>{}));
   count_launch();
   return LASER_OK;
 }
@@ -553,8 +710,9 @@ laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t strea
 
 int attention_int4_max_groups() { return kMaxSeqs; }
 size_t attention_int4_part_floats(int head_dim, int ctas) {
-  auto of = [&](auto z) { return size_t(ctas) * (2 * decltype(z)::kWarps + 2) * decltype(z)::kRecord; };
-  return head_dim == 128 ? std::max(of(Sizes<128, true>{}), of(Sizes<128, false>{})) : std::max(of(Sizes<64, true>{}), of(Sizes<64, false>{}));
+  auto most = [&](auto... z) { return std::max({decltype(z)::part_floats(ctas)...}); };
+  return head_dim == 128 ? most(Sizes<128, 1>{}, Sizes<128, 2>{}, Sizes<128, 3>{}, Sizes<128, 4>{}, Sizes<128, 5>{})
+                         : most(Sizes<64, 1>{}, Sizes<64, 2>{}, Sizes<64, 3>{}, Sizes<64, 4>{}, Sizes<64, 5>{});
 }
 
 laser_status attention_int4_launch(laser_model* m, laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* parents, int B, int Rs,

@@ -376,8 +376,8 @@ def test_offsets_beyond_32_bits(L):
 
 def test_many_sequences_in_a_call(L):
     rng = np.random.default_rng(13)
-    kv = make(L, 1, 1, 64, 2048, 2)
-    B = 2048
+    kv = make(L, 1, 1, 64, 1024, 2)
+    B = 1024
     lens = rng.integers(0, 31, B)
     n = rng.integers(0, 2, B)
     x = bf(rng.standard_normal((B * 32, 64)))
@@ -393,7 +393,7 @@ def test_many_sequences_in_a_call(L):
     check_rows(got[:64], f64(q)[:64], held, lens[:64].tolist(), n[:64].tolist(), None)
     assert (got[n == 0] == 2).all() and (got[64:][n[64:] == 1] == 0).all()      # (fresh pages hold zeros)
     with pytest.raises(L.LaserError) as e:
-        L.attend_int4(kv, 0, dev_i32([0] * 2049), dev_i32([0] * 2049), torch.zeros(2049, 1, 1, 64, dtype=torch.bfloat16, device="cuda"))
+        L.attend_int4(kv, 0, dev_i32([0] * 1025), dev_i32([0] * 1025), torch.zeros(1025, 1, 1, 64, dtype=torch.bfloat16, device="cuda"))
     assert e.value.status == -4
 
 
