@@ -6,8 +6,8 @@
 //
 // A CTA takes a run of the vocabulary for all rows of one sequence.  It counts the text's tokens of its run in shared memory (whole
 // numbers, whose order does not matter), notes which rows' tokens a token is as a 64-bit mask, and adds up its biases in the order of the
-// list; then a thread holds what it needs of its tokens in registers and the rows pass by: one load and one store a logit, coalesced
-// whatever the rows' alignment.  A warp's 32 tokens are one word of the grammar mask, and logits that it forbids are not read.
+// list; then the rows pass by: one load and one store a logit, coalesced whatever the rows' alignment, and the tables only where a token
+// has an entry.  A warp's 32 tokens are one word of the grammar mask, and logits that it forbids are not read.
 // Bound by memory where rows are many; with few rows by the counting (each CTA reads the text) and the launch.
 #include "model.cuh"
 #include "tree.cuh"
@@ -99,45 +99,61 @@ adjust_kernel(const AdjustArgs a) {
     }
   }
   __syncthreads();
-  uint32_t count[U], some = 0;
-  unsigned long long rows[U];
-  float bias[U];
+  uint32_t some = 0, inside = 0;      // of the thread's tokens: those that something is done to; those of the vocabulary
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    count[k] = s_count[k * kThreads + tid];
-    rows[k] = s_rows[k * kThreads + tid];
-    bias[k] = s_bias[k * kThreads + tid];
-    if (count[k] != 0 || rows[k] != 0 || bias[k] != 0.f) some |= 1u << k;      // (a NaN is some bias)
+    const int at = k * kThreads + tid;
+    if (s_count[at] != 0 || s_rows[at] != 0 || s_bias[at] != 0.f) some |= 1u << k;      // (a NaN is some bias)
+    if (v0 + at < a.V) inside |= 1u << k;
   }
   const float rep = a.repetition ? a.repetition[b] : 1.f, freq = a.frequency ? a.frequency[b] : 0.f, pres = a.presence ? a.presence[b] : 0.f;
-  for (int i = 0; i < nr; ++i) {
-    const size_t at = (size_t(b) * a.R + i) * a.V;
-    const uint32_t* words = a.allowed ? a.allowed + b * a.mask_seq_stride + i * a.mask_row_stride : nullptr;
-    uint32_t on = 0;
-    float x[U];
+  // a row's logits are requested while the one before is finished, its words of the mask one row earlier still (lane k: the warp's k-th word)
+  const float* in = a.logits + size_t(b) * a.R * a.V + v0 + tid;
+  float* out = a.out + size_t(b) * a.R * a.V + v0 + tid;
+  const int word = (v0 >> 5) + lane * (kThreads / 32) + (tid >> 5);
+  const bool has_word = a.allowed && lane < U && (word << 5) < a.V;
+  const uint32_t* words = a.allowed + b * a.mask_seq_stride + word;
+  auto mask = [&](int i) { return has_word && i < nr ? words[i * a.mask_row_stride] : 0u; };
+  auto fetch = [&](const float* from, uint32_t w, uint32_t& on, float (&x)[U]) {
+    on = inside;
+    if (a.allowed) {
+      uint32_t bits = 0;
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const int v = v0 + k * kThreads + tid;
-      bool ok = v < a.V;
-      if (words && ok) ok = words[v >> 5] >> lane & 1u;       // (v is lane mod 32)
-      if (ok) on |= 1u << k;
+      for (int k = 0; k < U; ++k) bits |= (__shfl_sync(0xffffffffu, w, k) >> lane & 1u) << k;      // (a token is lane mod 32)
+      on &= bits;
     }
 #pragma unroll
-    for (int k = 0; k < U; ++k) x[k] = on >> k & 1u ? a.logits[at + (v0 + k * kThreads + tid)] : -INFINITY;
+    for (int k = 0; k < U; ++k) x[k] = on >> k & 1u ? from[k * kThreads] : -INFINITY;
+  };
+  uint32_t next_word = mask(0), on, next_on = 0;
+  float x[U], next[U];
+  fetch(in, next_word, on, x);
+  next_word = mask(1);
+  for (int i = 0; i < nr; ++i) {
+    in += a.V;
+    if (i + 1 < nr) {
+      fetch(in, next_word, next_on, next);
+      next_word = mask(i + 2);
+    }
     if (some & on) {
       const unsigned long long path = s_path[i];
 #pragma unroll
       for (int k = 0; k < U; ++k) {
         if (!((some & on) >> k & 1u)) continue;
-        const int drafts = __popcll(rows[k] & path), n = int(count[k] & 0x7fffffffu) + drafts;
-        if (count[k] != 0 || drafts != 0) x[k] = x[k] > 0.f ? __fdiv_rn(x[k], rep) : __fmul_rn(x[k], rep);
+        const uint32_t count = s_count[k * kThreads + tid];
+        const int drafts = __popcll(s_rows[k * kThreads + tid] & path), n = int(count & 0x7fffffffu) + drafts;
+        if (count != 0 || drafts != 0) x[k] = x[k] > 0.f ? __fdiv_rn(x[k], rep) : __fmul_rn(x[k], rep);
         if (n > 0) x[k] = __fsub_rn(__fsub_rn(x[k], __fmul_rn(freq, float(n))), pres);
-        x[k] = __fadd_rn(x[k], bias[k]);
+        x[k] = __fadd_rn(x[k], s_bias[k * kThreads + tid]);
       }
     }
 #pragma unroll
     for (int k = 0; k < U; ++k)
-      if (v0 + k * kThreads + tid < a.V) a.out[at + (v0 + k * kThreads + tid)] = x[k];
+      if (inside >> k & 1u) out[k * kThreads] = x[k];
+    out += a.V;
+#pragma unroll
+    for (int k = 0; k < U; ++k) x[k] = next[k];
+    on = next_on;
   }
 }
 

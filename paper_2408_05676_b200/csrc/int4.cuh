@@ -41,7 +41,13 @@ __device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_fl
 
 // Scale and zero of the group that eight lanes (aligned, four features each) hold.
 struct Q4Scale { uint32_t s, z; };
-__device__ __forceinline__ float q4_finite(float x) { return x == x ? fminf(fmaxf(x, -kQ4Top), kQ4Top) : 0.f; }
+// NaN to 0, magnitudes to 2^124; a warp that has neither passes by
+__device__ __forceinline__ void q4_finite(float (&x)[4]) {
+  const bool fine = fabsf(x[0]) <= kQ4Top && fabsf(x[1]) <= kQ4Top && fabsf(x[2]) <= kQ4Top && fabsf(x[3]) <= kQ4Top;
+  if (__all_sync(0xffffffffu, fine)) return;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) x[u] = x[u] == x[u] ? fminf(fmaxf(x[u], -kQ4Top), kQ4Top) : 0.f;
+}
 __device__ __forceinline__ Q4Scale q4_scale(const float (&x)[4]) {
   float lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
 #pragma unroll
@@ -55,10 +61,25 @@ __device__ __forceinline__ Q4Scale q4_scale(const float (&x)[4]) {
   q.z = bf16_bits(__fsub_rn(lo, 16.f * bf16_value(q.s)));
   return q;
 }
-__device__ __forceinline__ uint32_t q4_code(float x, const Q4Scale& q) {
-  const float s = bf16_value(q.s);
-  if (q.s == 0) return 0;
-  return uint32_t(fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x, bf16_value(q.z)), s)) - 16.f, 0.f), 15.f));
+// The codes of four values.  The quotient is the rounded one's neighbour at most (31 x 2^-22); where that could decide between two codes
+// the division itself is made.
+__device__ __forceinline__ void q4_codes(const float (&x)[4], const Q4Scale& q, uint32_t (&code)[4]) {
+  const float s = bf16_value(q.s), z = bf16_value(q.z);
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  bool clear = true;
+  float v[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    v[u] = __fsub_rn(x[u], z) * inv;
+    clear = clear && fabsf(fabsf(v[u] - rintf(v[u])) - 0.5f) > 4e-5f;
+  }
+  if (!clear) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = __fdiv_rn(__fsub_rn(x[u], z), s);
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) code[u] = q.s == 0 ? 0u : uint32_t(fminf(fmaxf(rintf(v[u]) - 16.f, 0.f), 15.f));
 }
 // (the product is exact: eight and five bits)
 __device__ __forceinline__ uint32_t q4_held(uint32_t code, const Q4Scale& q) {

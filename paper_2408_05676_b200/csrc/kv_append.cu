@@ -5,8 +5,8 @@
 // position x theta^(-2j / dh); angles in 64 bits, since fp32 products are off by 1e-2 rad at position 1e5, the rotation itself in fp32.
 // A block takes one row and a share of its heads, so that a row's sines are worked out once per block; a lane holds four features
 // (8 or 16 bytes a load), head_dim / 4 lanes a head, the rotation's partner and a group's extremes come by shuffles.
-#include <cmath>
-#include <vector>
+#include <algorithm>
+#include <type_traits>
 
 #include "int4.cuh"
 #include "model.cuh"
@@ -16,6 +16,7 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kAppendThreads = 256;
+constexpr int kRowsMost = 8;      // rows of a block
 
 struct AppendArgs {
   // rows: from a step's tables (row_pos: slot, -1 = none; rope), or from the sequences' lengths, or a run of one sequence (run_seq >= 0)
@@ -25,6 +26,8 @@ struct AppendArgs {
   const double* inv_freq;
   int32_t* status;
   int run_seq, run_pos, Rs, max_seqs, capacity;
+  long long total;              // rows
+  int per_block;                // of them a block's
   int H, Hkv;
   const void *q, *k, *v;
   long long ldq, ldk, ldv;      // elements between rows
@@ -36,139 +39,175 @@ struct AppendArgs {
   uint8_t* pages4;
 };
 
+// Four features of a lane as they came, fetched before they are needed.
+template <typename T> struct Raw { T x[4]; };
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, int vec, float (&x)[4]) {
+__device__ __forceinline__ Raw<T> fetch4(const T* p, int vec) {
+  Raw<T> r;
   if (vec) {
-    if (sizeof(T) == 2) {
-      const uint2 u = *reinterpret_cast<const uint2*>(p);
-      x[0] = bf16_value(u.x & 0xffffu); x[1] = bf16_value(u.x >> 16);
-      x[2] = bf16_value(u.y & 0xffffu); x[3] = bf16_value(u.y >> 16);
-    } else {
-      const float4 f = *reinterpret_cast<const float4*>(p);
-      x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
-    }
+    if (sizeof(T) == 2) *reinterpret_cast<uint2*>(&r) = *reinterpret_cast<const uint2*>(p);
+    else *reinterpret_cast<uint4*>(&r) = *reinterpret_cast<const uint4*>(p);
   } else {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = float(p[u]);
+    for (int u = 0; u < 4; ++u) r.x[u] = p[u];
   }
+  return r;
 }
 
 template <typename T, int DH>
 __global__ void __launch_bounds__(kAppendThreads)
 kv_append_kernel(const AppendArgs a) {
   constexpr int LPH = DH / 4, HPW = 32 / LPH;       // lanes of a head, heads of a warp
-  __shared__ float2 s_cs[DH / 2];
-  __shared__ int s_par[64], s_depth;
+  constexpr int W = kAppendThreads / 32;
+  __shared__ float2 s_cs[kRowsMost][DH / 2];
+  __shared__ int s_par[64], s_pos[kRowsMost];       // a row's position
+  __shared__ void* s_dst[kRowsMost];          // its page (null: the row is not one)
+  __shared__ int s_slot[kRowsMost];                 // its place in the page
   next_may_launch();
-  const long long r = blockIdx.x;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l = lane % LPH;
+  const long long row0 = (long long)blockIdx.x * a.per_block;
+  const int here = int(min((long long)a.per_block, a.total - row0));
   wait_for_earlier();
-  int slot, seq, rpos;
-  if (a.row_pos) {
-    slot = a.row_pos[r]; seq = a.row_seq[r];
-    if (slot < 0) return;
-    if (tid < DH / 2) s_cs[tid] = *reinterpret_cast<const float2*>(a.rope + (size_t(r) * (DH / 2) + tid) * 2);
-  } else if (a.run_seq >= 0) {
-    seq = a.run_seq; slot = a.run_pos + int(r);
-  } else {
-    const int b = int(r / a.Rs), i = int(r % a.Rs);
-    seq = a.seq_ids[b];
-    const int nr = min(max(a.n_rows[b], 0), a.Rs);
-    if (i >= nr) return;
-    if (seq < 0 || seq >= a.max_seqs) {
-      if (tid == 0) atomicCAS(a.status, 0, LASER_ERR_INVALID_ARG);
-      return;
-    }
-    const int ctx = a.seq_len[seq];
-    if (ctx < 0 || nr > a.capacity - ctx) {
-      if (tid == 0) atomicCAS(a.status, 0, LASER_ERR_CAPACITY);
-      return;
-    }
-    slot = ctx + i;
-    rpos = slot;
-    if (a.parents) {              // (at most 64 rows, checked on the host)
-      if (tid <= i) s_par[tid] = a.parents[size_t(b) * a.Rs + tid];
-      __syncthreads();
-      if (tid == 0) {
-        int depth = 0;
-        for (int j = i; j > 0; ++depth) {     // parents are earlier rows: at most i steps
-          const int pj = s_par[j];
-          if (pj < 0 || pj >= j) { atomicCAS(a.status, 0, LASER_ERR_INVALID_ARG); break; }
-          j = pj;
+
+  // ---- the rows: a thread each ----
+  if (tid < here) {
+    const long long r = row0 + tid;
+    int slot = -1, seq = 0, pos = 0;
+    if (a.row_pos) {
+      slot = a.row_pos[r]; seq = a.row_seq[r];
+    } else if (a.run_seq >= 0) {
+      seq = a.run_seq; slot = a.run_pos + int(r);
+    } else {
+      const int b = int(r / a.Rs), i = int(r - (long long)b * a.Rs);
+      seq = a.seq_ids[b];
+      const int nr = min(max(a.n_rows[b], 0), a.Rs);
+      if (i < nr) {
+        if (seq < 0 || seq >= a.max_seqs) {
+          atomicCAS(a.status, 0, LASER_ERR_INVALID_ARG);
+        } else {
+          const int ctx = a.seq_len[seq];
+          if (ctx < 0 || nr > a.capacity - ctx) {
+            atomicCAS(a.status, 0, LASER_ERR_CAPACITY);
+          } else {
+            slot = pos = ctx + i;
+            if (a.parents) {
+              int depth = 0;
+              for (int j = i; j > 0; ++depth) {     // parents are earlier rows: at most i steps
+                const int pj = a.parents[size_t(b) * a.Rs + j];
+                if (pj < 0 || pj >= j) { atomicCAS(a.status, 0, LASER_ERR_INVALID_ARG); break; }
+                j = pj;
+              }
+              pos = ctx + depth;
+            }
+          }
         }
-        s_depth = depth;
       }
-      __syncthreads();
-      rpos = ctx + s_depth;
     }
-    if (tid < DH / 2) {
-      double s, c;
-      sincos(double(rpos) * a.inv_freq[tid], &s, &c);
-      s_cs[tid] = make_float2(float(c), float(s));
+    s_pos[tid] = pos;
+    s_slot[tid] = slot & 15;
+    void* dst = nullptr;
+    if (slot >= 0) {
+      const size_t page = size_t(a.page_table[size_t(seq) * a.pages_per_seq + (slot >> 4)]);
+      dst = a.pages4 ? static_cast<void*>(a.pages4 + page * a.Hkv * q4_block_bytes(DH)) : static_cast<void*>(a.pages + page * 2 * a.Hkv * 16 * DH);
     }
+    s_dst[tid] = dst;
   }
   __syncthreads();
-  const int page = a.page_table[size_t(seq) * a.pages_per_seq + (slot >> 4)], t = slot & 15;
-  const int heads = a.H + 2 * a.Hkv, items = (heads + HPW - 1) / HPW;
-  for (int it = blockIdx.y * (kAppendThreads / 32) + warp; it < items; it += gridDim.y * (kAppendThreads / 32)) {
-    const int hd = it * HPW + lane / LPH;
-    const bool live = hd < heads;
-    const int kind = !live ? -1 : hd < a.H ? 0 : hd < a.H + a.Hkv ? 1 : 2, h = kind == 0 ? hd : kind == 1 ? hd - a.H : hd - a.H - a.Hkv;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (live) {
-      const T* src = static_cast<const T*>(kind == 0 ? a.q : kind == 1 ? a.k : a.v) + r * (kind == 0 ? a.ldq : kind == 1 ? a.ldk : a.ldv);
-      load4(src + h * DH + 4 * l, a.vec, x);
-    }
-    float y[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float p = __shfl_xor_sync(0xffffffffu, x[u], LPH / 2);
-      y[u] = x[u];
-      if (a.run_seq < 0 && kind != 2) {
-        const float2 cs = s_cs[(4 * l + u) & (DH / 2 - 1)];
-        const float xc = __fmul_rn(x[u], cs.x), ps = __fmul_rn(p, cs.y);
-        y[u] = l < LPH / 2 ? __fsub_rn(xc, ps) : __fadd_rn(xc, ps);
+  // ---- their angles ----
+  if (a.run_seq < 0) {
+    for (int x = tid; x < here * (DH / 2); x += kAppendThreads) {
+      const int rr = x / (DH / 2), j = x % (DH / 2);
+      if (!s_dst[rr]) continue;
+      if (a.row_pos) {
+        s_cs[rr][j] = *reinterpret_cast<const float2*>(a.rope + (size_t(row0 + rr) * (DH / 2) + j) * 2);
+      } else {
+        double s, c;
+        sincos(double(s_pos[rr]) * a.inv_freq[j], &s, &c);
+        s_cs[rr][j] = make_float2(float(c), float(s));
       }
     }
-    uint32_t held[4];
-    if (a.pages4) {
-      if (kind > 0) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) y[u] = q4_finite(y[u]);
-      }
-      const Q4Scale sc = q4_scale(y);               // (all lanes take part; a query's is not used)
-      uint32_t code[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) { code[u] = q4_code(y[u], sc); held[u] = q4_held(code[u], sc); }
-      uint32_t kw = code[0] << 3 | code[1] << 19 | code[2] << 7 | code[3] << 23;
-      if (l & 1) kw = __funnelshift_l(kw, kw, 8);
-      kw |= __shfl_xor_sync(0xffffffffu, kw, 1);
-      uint8_t* blk = a.pages4 + (size_t(page) * a.Hkv + h) * q4_block_bytes(DH);
-      if (kind == 1) {
-        if (!(l & 1)) *reinterpret_cast<uint32_t*>(blk + q4_k_codes(DH, t, l >> 1)) = kw;
-        if (!(l & 7)) *reinterpret_cast<uint32_t*>(blk + q4_k_scale(DH, t, l >> 3)) = sc.s | sc.z << 16;
-      } else if (kind == 2) {
-        *reinterpret_cast<uint16_t*>(blk + q4_v_codes(DH, t, l)) = uint16_t(code[0] | code[1] << 4 | code[2] << 8 | code[3] << 12);
-        if (!(l & 7)) {
-          uint8_t* p = blk + q4_v_scale(DH, t, l >> 3);
-          *reinterpret_cast<uint16_t*>(p) = uint16_t(sc.s);
-          *reinterpret_cast<uint16_t*>(p + 4) = uint16_t(sc.z);
-        }
-      }
-      if (kind == 0) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) held[u] = bf16_bits(y[u]);
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) held[u] = bf16_bits(y[u]);
-    }
-    const uint2 out = make_uint2(held[0] | held[1] << 16, held[2] | held[3] << 16);
-    if (!a.pages4 && kind > 0)
-      *reinterpret_cast<uint2*>(a.pages + (size_t(page) * 2 * a.Hkv + size_t(kind - 1) * a.Hkv + h) * 16 * DH + t * DH + 4 * l) = out;
-    bf16* dst = kind == 0 ? a.q_out : kind == 1 ? a.k_out : kind == 2 ? a.v_out : nullptr;
-    if (dst) *reinterpret_cast<uint2*>(dst + (size_t(r) * (kind == 0 ? a.H : a.Hkv) + h) * DH + 4 * l) = out;
+    __syncthreads();
   }
+
+  // ---- a warp takes a share of one row's heads, one (or two of 64) at a time, kAhead of them on their way together ----
+  const int warps_of_row = W / a.per_block, rr = warp / warps_of_row;
+  if (rr >= here || !s_dst[rr]) return;
+  const int part = blockIdx.y * warps_of_row + warp % warps_of_row, parts = gridDim.y * warps_of_row;
+  const long long r = row0 + rr;
+  const int t = s_slot[rr];
+  uint8_t* const page = static_cast<uint8_t*>(s_dst[rr]);
+  float cs[4], sn[4];        // the lane's sines, with the sign that its half of the head takes them with
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float2 x = s_cs[rr][(4 * l + u) & (DH / 2 - 1)];
+    cs[u] = x.x;
+    sn[u] = l < LPH / 2 ? -x.y : x.y;
+  }
+  constexpr int kAhead = 4;
+  auto heads = [&](auto kind_tag, const T* src, int count, bf16* to) {
+    constexpr int kKind = decltype(kind_tag)::value;       // 0 = q, 1 = k, 2 = v
+    const int hl = lane / LPH;
+    for (int h0 = part * HPW; h0 < count; h0 += kAhead * parts * HPW) {
+      Raw<T> raw[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int h = h0 + u * parts * HPW + hl;
+        raw[u] = h < count ? fetch4(src + h * DH + 4 * l, a.vec) : Raw<T>{};
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (h0 + u * parts * HPW >= count) break;
+        const int h = h0 + u * parts * HPW + hl;
+        const bool live = h < count;
+        float y[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = float(raw[u].x[c]);
+        if (kKind != 2 && a.run_seq < 0) {
+          float p[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) p[c] = __shfl_xor_sync(0xffffffffu, y[c], LPH / 2);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) y[c] = __fadd_rn(__fmul_rn(y[c], cs[c]), __fmul_rn(p[c], sn[c]));
+        }
+        uint32_t held[4];
+        if (kKind == 0 || !a.pages4) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) held[c] = bf16_bits(y[c]);
+          if (kKind > 0 && live)
+            *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(page) + (size_t(kKind - 1) * a.Hkv + h) * 16 * DH + t * DH + 4 * l) =
+                make_uint2(held[0] | held[1] << 16, held[2] | held[3] << 16);
+        } else {
+          q4_finite(y);
+          const Q4Scale sc = q4_scale(y);
+          uint32_t code[4];
+          q4_codes(y, sc, code);
+          uint8_t* blk = page + h * q4_block_bytes(DH);
+          if (kKind == 1) {
+            uint32_t kw = code[0] << 3 | code[1] << 19 | code[2] << 7 | code[3] << 23;
+            if (l & 1) kw = __funnelshift_l(kw, kw, 8);
+            kw |= __shfl_xor_sync(0xffffffffu, kw, 1);
+            if (live && !(l & 1)) *reinterpret_cast<uint32_t*>(blk + q4_k_codes(DH, t, l >> 1)) = kw;
+            if (live && !(l & 7)) *reinterpret_cast<uint32_t*>(blk + q4_k_scale(DH, t, l >> 3)) = sc.s | sc.z << 16;
+          } else if (live) {
+            *reinterpret_cast<uint16_t*>(blk + q4_v_codes(DH, t, l)) = uint16_t(code[0] | code[1] << 4 | code[2] << 8 | code[3] << 12);
+            if (!(l & 7)) {
+              uint8_t* p = blk + q4_v_scale(DH, t, l >> 3);
+              *reinterpret_cast<uint16_t*>(p) = uint16_t(sc.s);
+              *reinterpret_cast<uint16_t*>(p + 4) = uint16_t(sc.z);
+            }
+          }
+          if (to) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) held[c] = q4_held(code[c], sc);
+          }
+        }
+        if (to && live) *reinterpret_cast<uint2*>(to + (size_t(r) * count + h) * DH + 4 * l) = make_uint2(held[0] | held[1] << 16, held[2] | held[3] << 16);
+      }
+    }
+  };
+  heads(std::integral_constant<int, 1>{}, static_cast<const T*>(a.k) + r * a.ldk, a.Hkv, a.k_out);
+  heads(std::integral_constant<int, 2>{}, static_cast<const T*>(a.v) + r * a.ldv, a.Hkv, a.v_out);
+  if (a.H) heads(std::integral_constant<int, 0>{}, static_cast<const T*>(a.q) + r * a.ldq, a.H, a.q_out);
 }
 
 // What a 4-bit cache holds of tokens [pos0, pos0 + n) of one sequence, as bf16: a thread takes four features of K or V.
@@ -238,12 +277,15 @@ __global__ void compact_path_q4_kernel(uint8_t* __restrict__ pages, size_t layer
   }
 }
 
-laser_status launch_append(const AppendArgs& a, int64_t rows, int dh, int dtype, cudaStream_t stream) {
-  // a row's heads are shared out while that gives the GPU's SMs more blocks
-  const int items = ceil_div(a.H + 2 * a.Hkv, 128 / dh), warps = kAppendThreads / 32;
-  const int parts = int(std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, warps), 592 / std::max<int64_t>(rows, 1))));
+laser_status launch_append(AppendArgs a, int64_t rows, int dh, int dtype, cudaStream_t stream) {
+  // a row a warp where rows are many; where they are few, up to eight warps a row and several blocks
+  const int heads = std::max(a.H, a.Hkv), items = ceil_div(heads, 128 / dh), warps = kAppendThreads / 32;
+  a.total = rows;
+  a.per_block = rows >= 592 * 8 ? 8 : rows >= 592 * 4 ? 4 : rows >= 592 * 2 ? 2 : 1;
+  const int64_t blocks = ceil_div(rows, int64_t(a.per_block));
+  const int parts = int(std::max<int64_t>(1, std::min<int64_t>(ceil_div(items * a.per_block, warps), 592 / blocks)));
   auto launch = [&](auto kernel) -> laser_status {
-    LASER_CUDA(launch_overlapped(kernel, dim3(unsigned(rows), unsigned(parts)), kAppendThreads, 0, stream, a));
+    LASER_CUDA(launch_overlapped(kernel, dim3(unsigned(blocks), unsigned(parts)), kAppendThreads, 0, stream, a));
     return LASER_OK;
   };
   if (dtype == LASER_DTYPE_F32) LASER_TRY(dh == 128 ? launch(kv_append_kernel<float, 128>) : launch(kv_append_kernel<float, 64>));
