@@ -327,17 +327,35 @@ def kv_create_int4(model: Model, max_seqs: int, n_pages: int) -> KV:
     return KV(h, model, max_seqs, n_pages)
 
 
-def _rows_at(t: torch.Tensor, dtype, B: int, rows: int, width: int):
+_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+
+
+def _adr(t, dtype, shape, dev: int) -> int:
+    """The address of a contiguous tensor of that type and shape on the given GPU."""
+    if not (t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev):
+        raise AssertionError("expected a contiguous %s %s on cuda:%d, not %s %s on %s" % (dtype, tuple(shape), dev, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _home(t, stream):
+    """The GPU of a call's tensors, and its stream: the launch goes to the current device, so they have to be there."""
+    dev = t.get_device()
+    if stream is not None:
+        return dev, _stream_at(stream)
+    if dev != torch._C._cuda_getDevice():
+        raise AssertionError("tensors on cuda:%d, the current device is cuda:%d" % (dev, torch._C._cuda_getDevice()))
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _rows_at(t, dtype, B: int, rows: int, width: int, dev: int):
     """Address and row stride (in elements) of [B, rows, ..] rows of `width` adjacent elements on the GPU, which may lie apart."""
-    assert t.is_cuda and t.dtype == dtype, (t.device, t.dtype, dtype)
-    sizes, strides = t.shape, t.stride()
-    assert sizes[0] == B and sizes[1] == rows, (tuple(sizes), B, rows)
-    if len(sizes) == 3:
-        assert sizes[2] == width and strides[2] == 1, (tuple(sizes), strides, width)
-    else:
-        assert len(sizes) == 4 and sizes[2] * sizes[3] == width and strides[3] == 1 and strides[2] == sizes[3], (tuple(sizes), strides, width)
-    ld = strides[1] if rows > 1 else strides[0] if B > 1 else width
-    assert B == 1 or strides[0] == rows * ld, "rows must be evenly spaced"
+    n, st = t.shape, t.stride()
+    ok = t.is_cuda and t.dtype is dtype and t.get_device() == dev and n[0] == B and n[1] == rows
+    ok = ok and (n[2] == width and st[2] == 1 if len(n) == 3 else len(n) == 4 and n[2] * n[3] == width and st[3] == 1 and st[2] == n[3])
+    ld = st[1] if rows > 1 else st[0] if B > 1 else width
+    if not (ok and (B == 1 or st[0] == rows * ld)):
+        raise AssertionError("expected evenly spaced rows [%d, %d, %d] of %s on cuda:%d, not %s with strides %s, %s on %s"
+                             % (B, rows, width, dtype, dev, tuple(n), st, t.dtype, t.device))
     return t.data_ptr(), ld
 
 
@@ -347,19 +365,25 @@ def kv_append(kv: KV, layer: int, seq_ids, n_rows, k, v, q=None, parents=None, q
     the cache now holds."""
     cfg = kv.model.cfg
     H, Hkv, dh = cfg["n_heads"], cfg["n_kv_heads"], cfg["head_dim"]
-    B, rows = k.shape[0], k.shape[1]
-    assert k.dtype in (torch.bfloat16, torch.float32), k.dtype
-    assert seq_ids.shape == (B,) and n_rows.shape == (B,) and (parents is None or parents.shape == (B, rows))
-    (ka, ks), (va, vs) = _rows_at(k, k.dtype, B, rows, Hkv * dh), _rows_at(v, k.dtype, B, rows, Hkv * dh)
-    qa, qs = (0, 0) if q is None else _rows_at(q, k.dtype, B, rows, H * dh)
-    if q is not None and q_out is None:
-        q_out = torch.empty(B, rows, H, dh, dtype=torch.bfloat16, device=k.device)
-    assert q_out is None or q_out.numel() == B * rows * H * dh
-    assert all(t is None or t.numel() == B * rows * Hkv * dh for t in (k_out, v_out))
-    out = [0 if t is None else _at(t, torch.bfloat16) for t in (q_out, k_out, v_out)]
-    _chk(lib.laser_kv_append(kv.handle, layer, _at(seq_ids, torch.int32), None if parents is None else _at(parents, torch.int32),
-                             _at(n_rows, torch.int32), B, rows, 0 if k.dtype == torch.bfloat16 else 1, qa, qs, ka, ks, va, vs, *out,
-                             _stream_at(stream)))
+    n = k.shape
+    B, rows, dtype = n[0], n[1], k.dtype
+    assert dtype is _BF16 or dtype is _F32, dtype
+    dev, st = _home(k, stream)
+    ka, ks = _rows_at(k, dtype, B, rows, Hkv * dh, dev)
+    va, vs = _rows_at(v, dtype, B, rows, Hkv * dh, dev)
+    qa = qs = qo = 0
+    if q is not None:
+        qa, qs = _rows_at(q, dtype, B, rows, H * dh, dev)
+        if q_out is None:
+            q_out = torch.empty(B, rows, H, dh, dtype=_BF16, device=k.device)
+    if q_out is not None:
+        qo = _adr(q_out, _BF16, (B, rows, H, dh), dev)
+    held = (B, rows, Hkv, dh)
+    status = lib.laser_kv_append(kv.handle, layer, _adr(seq_ids, _I32, (B,), dev), None if parents is None else _adr(parents, _I32, (B, rows), dev),
+                                 _adr(n_rows, _I32, (B,), dev), B, rows, 0 if dtype is _BF16 else 1, qa, qs, ka, ks, va, vs, qo,
+                                 None if k_out is None else _adr(k_out, _BF16, held, dev), None if v_out is None else _adr(v_out, _BF16, held, dev), st)
+    if status:
+        _chk(status)
     return q_out
 
 
@@ -368,13 +392,17 @@ def attend_int4(kv: KV, layer: int, seq_ids, n_rows, q, parents=None, out=None, 
     may those of out."""
     cfg = kv.model.cfg
     width = cfg["n_heads"] * cfg["head_dim"]
-    B, rows = q.shape[0], q.shape[1]
-    assert seq_ids.shape == (B,) and n_rows.shape == (B,) and (parents is None or parents.shape == (B, rows))
+    n = q.shape
+    B, rows = n[0], n[1]
+    dev, st = _home(q, stream)
     if out is None:
-        out = torch.empty(B, rows, cfg["n_heads"], cfg["head_dim"], dtype=torch.bfloat16, device=q.device)
-    (qa, qs), (oa, os_) = _rows_at(q, torch.bfloat16, B, rows, width), _rows_at(out, torch.bfloat16, B, rows, width)
-    _chk(lib.laser_attend_int4(kv.handle, layer, _at(seq_ids, torch.int32), None if parents is None else _at(parents, torch.int32),
-                               _at(n_rows, torch.int32), B, rows, qa, qs, oa, os_, _stream_at(stream)))
+        out = torch.empty(B, rows, cfg["n_heads"], cfg["head_dim"], dtype=_BF16, device=q.device)
+    qa, qs = _rows_at(q, _BF16, B, rows, width, dev)
+    oa, os_ = _rows_at(out, _BF16, B, rows, width, dev)
+    status = lib.laser_attend_int4(kv.handle, layer, _adr(seq_ids, _I32, (B,), dev), None if parents is None else _adr(parents, _I32, (B, rows), dev),
+                                   _adr(n_rows, _I32, (B,), dev), B, rows, qa, qs, oa, os_, st)
+    if status:
+        _chk(status)
     return out
 
 
@@ -483,25 +511,37 @@ def adjust_logits(logits, tokens, n_rows, hist=None, hist_len=None, prompt_len=N
                   parents=None, out=None, stream=None) -> torch.Tensor:
     """laser_adjust_logits: penalties = (repetition, frequency, presence), fp32 [B] or None each; bias = (offsets int32 [B + 1], ids int32,
     values fp32) or None; allowed int32 [B, rows or 1, words of 32 tokens] or None.  out may be logits."""
-    B, R, V = logits.shape
+    B, R, V = shape = logits.shape
+    dev, st = _home(logits, stream)
     if out is None:
         out = torch.empty_like(logits)
-    assert tokens.shape == (B, R) and out.shape == logits.shape and n_rows.shape == (B,) and (parents is None or parents.shape == (B, R))
-    assert (hist is None) == (hist_len is None), "hist and hist_len go together"
-    i32 = lambda t: None if t is None else _at(t, torch.int32)
-    f32 = lambda t: None if t is None else _at(t, torch.float32)
-    assert hist is None or (hist.dim() == 2 and hist.shape[0] == B and hist_len.shape == (B,))
-    assert all(t is None or t.shape == (B,) for t in (prompt_len, *penalties))
-    off, ids, val = bias if bias is not None else (None, None, None)
-    assert off is None or (off.shape == (B + 1,) and ids.shape == val.shape)
-    ss = rs = 0
+    one, rows = (B,), (B, R)
+    ha = hl = stride = pl = rep = freq = pres = off = ids = val = words = ss = rs = None
+    if hist is not None:
+        stride = hist.shape[1]
+        ha, hl = _adr(hist, _I32, (B, stride), dev), _adr(hist_len, _I32, one, dev)
+    if prompt_len is not None:
+        pl = _adr(prompt_len, _I32, one, dev)
+    r, f, p = penalties
+    if r is not None:
+        rep = _adr(r, _F32, one, dev)
+    if f is not None:
+        freq = _adr(f, _F32, one, dev)
+    if p is not None:
+        pres = _adr(p, _F32, one, dev)
+    if bias is not None:
+        o, i, v = bias
+        off, ids, val = _adr(o, _I32, (B + 1,), dev), _adr(i, _I32, v.shape, dev), _adr(v, _F32, i.shape, dev)
     if allowed is not None:
-        words = -(-V // 32)
-        assert allowed.dim() == 3 and allowed.shape[0] == B and allowed.shape[1] in (1, R) and allowed.shape[2] >= words, tuple(allowed.shape)
-        ss, rs = allowed.shape[1] * allowed.shape[2], allowed.shape[2] if allowed.shape[1] == R else 0
-    _chk(lib.laser_adjust_logits(_at(logits, torch.float32), _at(tokens, torch.int32), i32(parents), _at(n_rows, torch.int32), i32(hist),
-                                 i32(hist_len), 0 if hist is None else hist.shape[1], i32(prompt_len), *[f32(t) for t in penalties],
-                                 i32(off), i32(ids), f32(val), i32(allowed), ss, rs, B, R, V, _at(out, torch.float32), _stream_at(stream)))
+        n = allowed.shape
+        if len(n) != 3 or n[0] != B or (n[1] != 1 and n[1] != R) or 32 * n[2] < V:
+            raise AssertionError("allowed: %s for %d sequences of 1 or %d rows and %d tokens" % (tuple(n), B, R, V))
+        words, ss, rs = _adr(allowed, _I32, n, dev), n[1] * n[2], n[2] if n[1] == R else 0
+    status = lib.laser_adjust_logits(_adr(logits, _F32, shape, dev), _adr(tokens, _I32, rows, dev), None if parents is None else _adr(parents, _I32, rows, dev),
+                                     _adr(n_rows, _I32, one, dev), ha, hl, stride or 0, pl, rep, freq, pres, off, ids, val, words, ss or 0, rs or 0, B, R, V,
+                                     _adr(out, _F32, shape, dev), st)
+    if status:
+        _chk(status)
     return out
 
 

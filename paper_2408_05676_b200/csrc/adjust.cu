@@ -6,16 +6,19 @@
 //
 // A CTA takes a run of the vocabulary for all rows of one sequence.  It counts the text's tokens of its run in shared memory (whole
 // numbers, whose order does not matter), notes which rows' tokens a token is as a 64-bit mask, and adds up its biases in the order of the
-// list; then the rows pass by: one load and one store a logit, coalesced whatever the rows' alignment, and the tables only where a token
-// has an entry.  A warp's 32 tokens are one word of the grammar mask, and logits that it forbids are not read.
-// Bound by memory where rows are many; with few rows by the counting (each CTA reads the text) and the launch.
+// list; what that means for a row's logits is a factor and a difference a token, but for the step's own drafts.  Then the rows pass by, a
+// load and a store a logit, coalesced whatever the rows' alignment.  A trip to memory takes 1.6 us under load, so each thread has its
+// logits of the next kAhead rows on their way into shared memory (72 KB an SM; with one row ahead, in registers, 64 trees of 17 rows took
+// 71 us instead of 66).  A warp's 32 tokens are one word of the grammar mask, and logits that it forbids are not read.
 #include "model.cuh"
+#include "tma.cuh"
 #include "tree.cuh"
 
 namespace laser {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 3;
 
 struct AdjustArgs {
   const float* logits;
@@ -30,130 +33,192 @@ struct AdjustArgs {
   int R, V;
 };
 
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // U: tokens of a thread
 template <int U>
-__global__ void __launch_bounds__(kThreads)
+struct Tables {
+  static constexpr int C = U * kThreads;
+  unsigned long long rows[C];     // rows of the step whose token it is
+  uint32_t count[C];              // occurrences in the generated text; top bit: one in the prompt
+  float bias[C];
+  float x[kAhead][C];             // logits of the next rows
+  uint32_t words[2 * kAhead][C / 32];   // and their words of the mask, twice as far ahead
+  unsigned long long path[64];
+  int id[kThreads];
+  float val[kThreads];
+};
+
+template <int U>
+__global__ void __launch_bounds__(kThreads, 3)
 adjust_kernel(const AdjustArgs a) {
-  constexpr int C = U * kThreads;
-  __shared__ uint32_t s_count[C];              // occurrences in the generated text; top bit: one in the prompt
-  __shared__ unsigned long long s_rows[C];     // rows of the step whose token it is
-  __shared__ float s_bias[C];
-  __shared__ unsigned long long s_path[64];
-  __shared__ int s_id[kThreads];
-  __shared__ float s_val[kThreads];
+  using S = Tables<U>;
+  constexpr int C = S::C, kFirst = 4;
+  extern __shared__ __align__(16) uint8_t smem[];
+  S& s = *reinterpret_cast<S*>(smem);
   next_may_launch();
-  const int b = blockIdx.y, v0 = blockIdx.x * C, tid = threadIdx.x, lane = tid & 31;
+  const int b = blockIdx.y, v0 = blockIdx.x * C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 #pragma unroll
-  for (int k = 0; k < U; ++k) { s_count[k * kThreads + tid] = 0; s_rows[k * kThreads + tid] = 0; s_bias[k * kThreads + tid] = 0.f; }
+  for (int k = 0; k < U; ++k) { s.count[k * kThreads + tid] = 0; s.rows[k * kThreads + tid] = 0; s.bias[k * kThreads + tid] = 0.f; }
   wait_for_earlier();
-  const int nr = min(max(a.n_rows[b], 0), a.R);
+  // ---- what is read before the rows, in two trips to memory: the sequence's numbers and the first rows' words of the mask; then the first of
+  // its text, biases and drafts, and the first rows ----
+  const int word = lane * (kThreads / 32) + warp;                                          // a lane's word: the tokens k kThreads + 32 warp on, k = lane
+  const bool has_word = a.allowed && lane < U && v0 + (word << 5) < a.V;
+  const uint32_t* const words = a.allowed + b * a.mask_seq_stride + (v0 >> 5) + word;
+  auto get_words = [&](int i) { if (has_word && i < a.R) copy4(smem_u32(&s.words[i % (2 * kAhead)][word]), words + i * a.mask_row_stride); };
+#pragma unroll
+  for (int i = 0; i < 2 * kAhead; ++i) get_words(i);
+  copies_commit();
+  const int n_rows = a.n_rows[b];
+  const int hist_len = a.hist ? a.hist_len[b] : 0, made = a.prompt_len ? a.prompt_len[b] : 0;
+  const int bias_from = a.bias_offsets ? a.bias_offsets[b] : 0, bias_to = a.bias_offsets ? a.bias_offsets[b + 1] : 0;
+  const float rep = a.repetition ? a.repetition[b] : 1.f, freq = a.frequency ? a.frequency[b] : 0.f, pres = a.presence ? a.presence[b] : 0.f;
+  const int nr = min(max(n_rows, 0), a.R), len = int(min((long long)max(hist_len, 0), a.hist_stride));
+  copies_wait<0>();
   if (nr == 0) return;
-  __syncthreads();
-  if (tid < 32) {
-    unsigned long long mask[2];
+  __syncwarp();
+  uint32_t inside = 0;                         // the thread's tokens that are of the vocabulary
+#pragma unroll
+  for (int k = 0; k < U; ++k) if (v0 + k * kThreads + tid < a.V) inside |= 1u << k;
+  auto allowed = [&](int i) {                  // those that row i may have
+    if (!a.allowed) return inside;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int k = 0; k < U; ++k) bits |= (s.words[i % (2 * kAhead)][k * (kThreads / 32) + warp] >> lane & 1u) << k;      // (a token is lane mod 32)
+    return bits & inside;
+  };
+  const float* in = a.logits + size_t(b) * a.R * a.V + v0 + tid;      // of the next row to be requested
+  auto get_row = [&](int i) {
+    if (i < nr) {
+      const uint32_t on = allowed(i), at = smem_u32(&s.x[i % kAhead][tid]);
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (on >> k & 1u) copy4(at + k * (kThreads * 4), in + k * kThreads);
+    }
+    in += a.V;
+  };
+#pragma unroll 1
+  for (int i = 0; i < kAhead; ++i) {
+    get_row(i);
+    copies_commit();
+  }
+  const int32_t* const text = a.hist + size_t(b) * a.hist_stride;
+  int tok[kFirst];
+#pragma unroll
+  for (int u = 0; u < kFirst; ++u) tok[u] = tid + u * kThreads < len ? text[tid + u * kThreads] : -1;
+  const int draft = tid > 0 && tid < nr ? a.tokens[size_t(b) * a.R + tid] : -1;
+  int id = bias_from + tid < bias_to ? a.bias_ids[bias_from + tid] : -1;
+  float val = bias_from + tid < bias_to ? a.bias_values[bias_from + tid] : 0.f;
+  if (warp == 0) {
+    unsigned long long path[2];
     if (a.parents) {
-      tree_paths(a.parents + size_t(b) * a.R, nr, lane, mask);
+      tree_paths(a.parents + size_t(b) * a.R, nr, lane, path);
     } else {
-      mask[0] = (2ull << lane) - 1;
-      mask[1] = (2ull << (lane + 32)) - 1;     // (row 63: all ones)
+      path[0] = (2ull << lane) - 1;
+      path[1] = (2ull << (lane + 32)) - 1;     // (row 63: all ones)
     }
-    s_path[lane] = mask[0] & ~1ull;            // the pending token, row 0, is in the text
-    s_path[lane + 32] = mask[1] & ~1ull;
+    s.path[lane] = path[0] & ~1ull;            // the pending token, row 0, is in the text
+    s.path[lane + 32] = path[1] & ~1ull;
   }
-  const int len = a.hist ? int(min((long long)max(a.hist_len[b], 0), a.hist_stride)) : 0, made = a.prompt_len ? a.prompt_len[b] : 0;
-  const int32_t* text = a.hist + size_t(b) * a.hist_stride;
-#pragma unroll 4
-  for (int j = tid; j < len; j += kThreads) {
-    const unsigned at = unsigned(text[j]) - unsigned(v0);
+
+  // ---- the tables ----
+  __syncthreads();
+  auto count = [&](int token, int j) {
+    const unsigned at = unsigned(token) - unsigned(v0);
     if (at < unsigned(C)) {
-      if (j >= made) atomicAdd(&s_count[at], 1u);
-      else atomicOr(&s_count[at], 0x80000000u);
+      if (j >= made) atomicAdd(&s.count[at], 1u);
+      else atomicOr(&s.count[at], 0x80000000u);
     }
+  };
+#pragma unroll
+  for (int u = 0; u < kFirst; ++u) count(tok[u], tid + u * kThreads);
+#pragma unroll 4
+  for (int j = tid + kFirst * kThreads; j < len; j += kThreads) count(text[j], j);
+  {
+    const unsigned at = unsigned(draft) - unsigned(v0);
+    if (at < unsigned(C)) atomicOr(&s.rows[at], 1ull << tid);
   }
-  if (tid > 0 && tid < nr) {
-    const unsigned at = unsigned(a.tokens[size_t(b) * a.R + tid]) - unsigned(v0);
-    if (at < unsigned(C)) atomicOr(&s_rows[at], 1ull << tid);
-  }
-  if (a.bias_offsets) {
-    const int from = a.bias_offsets[b], to = a.bias_offsets[b + 1];
-    for (int j0 = from; j0 < to; j0 += kThreads) {
+  for (int j0 = bias_from; j0 < bias_to; j0 += kThreads) {
+    if (j0 > bias_from) {
       __syncthreads();
-      s_id[tid] = j0 + tid < to ? a.bias_ids[j0 + tid] : -1;
-      s_val[tid] = j0 + tid < to ? a.bias_values[j0 + tid] : 0.f;
-      __syncthreads();
-      if (tid < 32) {
-        for (int x = 0; x < min(kThreads, to - j0); x += 32) {
-          const int id = s_id[x + lane];
-          const unsigned at = unsigned(id) - unsigned(v0);
-          const bool here = id >= 0 && at < unsigned(C);
-          if (!__any_sync(0xffffffffu, here)) continue;
-          // entries of one token are added in the list's order
-          const unsigned same = __match_any_sync(0xffffffffu, here ? int(at) : -1);
-          const int turn = __popc(same & ((1u << lane) - 1)), turns = __reduce_max_sync(0xffffffffu, here ? turn : 0);
-          for (int y = 0; y <= turns; ++y) {
-            if (here && turn == y) s_bias[at] += s_val[x + lane];
-            __syncwarp();
-          }
+      id = j0 + tid < bias_to ? a.bias_ids[j0 + tid] : -1;
+      val = j0 + tid < bias_to ? a.bias_values[j0 + tid] : 0.f;
+    }
+    s.id[tid] = id;
+    s.val[tid] = val;
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll 1
+      for (int x0 = 0; x0 < min(kThreads, bias_to - j0); x0 += 32) {
+        const unsigned at = unsigned(s.id[x0 + lane]) - unsigned(v0);
+        const bool here = at < unsigned(C);
+        if (!__any_sync(0xffffffffu, here)) continue;
+        // entries of one token are added in the list's order
+        const unsigned same = __match_any_sync(0xffffffffu, here ? int(at) : -1);
+        const int turn = __popc(same & ((1u << lane) - 1)), turns = __reduce_max_sync(0xffffffffu, here ? turn : 0);
+        for (int y = 0; y <= turns; ++y) {
+          if (here && turn == y) s.bias[at] += s.val[x0 + lane];
+          __syncwarp();
         }
       }
     }
   }
   __syncthreads();
-  uint32_t some = 0, inside = 0;      // of the thread's tokens: those that something is done to; those of the vocabulary
+  // of the thread's tokens: those of the text, what is taken from them (all three terms as one), and those that are drafts, few
+  // enough for a branch
+  uint32_t seen = 0, drafted = 0;
+  float less[U];
 #pragma unroll
   for (int k = 0; k < U; ++k) {
     const int at = k * kThreads + tid;
-    if (s_count[at] != 0 || s_rows[at] != 0 || s_bias[at] != 0.f) some |= 1u << k;      // (a NaN is some bias)
-    if (v0 + at < a.V) inside |= 1u << k;
+    const uint32_t c = s.count[at];
+    const float n = float(c & 0x7fffffffu);
+    less[k] = (freq * n + (n > 0.f ? pres : 0.f)) - s.bias[at];
+    if (s.rows[at] != 0) { drafted |= 1u << k; less[k] = 0.f; }
+    else if (c != 0) seen |= 1u << k;
   }
-  const float rep = a.repetition ? a.repetition[b] : 1.f, freq = a.frequency ? a.frequency[b] : 0.f, pres = a.presence ? a.presence[b] : 0.f;
-  // a row's logits are requested while the one before is finished, its words of the mask one row earlier still (lane k: the warp's k-th word)
-  const float* in = a.logits + size_t(b) * a.R * a.V + v0 + tid;
+  const float inv = 1.f / rep;
+
+  // ---- the rows ----
   float* out = a.out + size_t(b) * a.R * a.V + v0 + tid;
-  const int word = (v0 >> 5) + lane * (kThreads / 32) + (tid >> 5);
-  const bool has_word = a.allowed && lane < U && (word << 5) < a.V;
-  const uint32_t* words = a.allowed + b * a.mask_seq_stride + word;
-  auto mask = [&](int i) { return has_word && i < nr ? words[i * a.mask_row_stride] : 0u; };
-  auto fetch = [&](const float* from, uint32_t w, uint32_t& on, float (&x)[U]) {
-    on = inside;
-    if (a.allowed) {
-      uint32_t bits = 0;
-#pragma unroll
-      for (int k = 0; k < U; ++k) bits |= (__shfl_sync(0xffffffffu, w, k) >> lane & 1u) << k;      // (a token is lane mod 32)
-      on &= bits;
-    }
-#pragma unroll
-    for (int k = 0; k < U; ++k) x[k] = on >> k & 1u ? from[k * kThreads] : -INFINITY;
-  };
-  uint32_t next_word = mask(0), on, next_on = 0;
-  float x[U], next[U];
-  fetch(in, next_word, on, x);
-  next_word = mask(1);
+#pragma unroll 1
   for (int i = 0; i < nr; ++i) {
-    in += a.V;
-    if (i + 1 < nr) {
-      fetch(in, next_word, next_on, next);
-      next_word = mask(i + 2);
+    copies_wait<kAhead - 1>();
+    __syncwarp();
+    const uint32_t on = allowed(i);
+    float x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      x[k] = s.x[i % kAhead][k * kThreads + tid];
+      const float f = x[k] > 0.f ? inv : rep, y = x[k] * (seen >> k & 1u ? f : 1.f) - less[k];
+      x[k] = on >> k & 1u ? y : -INFINITY;
     }
-    if (some & on) {
-      const unsigned long long path = s_path[i];
+    if (drafted & on) {
+      const unsigned long long path = s.path[i];
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        if (!((some & on) >> k & 1u)) continue;
-        const uint32_t count = s_count[k * kThreads + tid];
-        const int drafts = __popcll(s_rows[k * kThreads + tid] & path), n = int(count & 0x7fffffffu) + drafts;
-        if (count != 0 || drafts != 0) x[k] = x[k] > 0.f ? __fdiv_rn(x[k], rep) : __fmul_rn(x[k], rep);
-        if (n > 0) x[k] = __fsub_rn(__fsub_rn(x[k], __fmul_rn(freq, float(n))), pres);
-        x[k] = __fadd_rn(x[k], s_bias[k * kThreads + tid]);
+        if (!((drafted & on) >> k & 1u)) continue;
+        const uint32_t c = s.count[k * kThreads + tid];
+        const int drafts = __popcll(s.rows[k * kThreads + tid] & path);
+        const float n = float(int(c & 0x7fffffffu) + drafts);
+        if (c != 0 || drafts != 0) x[k] *= x[k] > 0.f ? inv : rep;
+        x[k] -= (freq * n + (n > 0.f ? pres : 0.f)) - s.bias[k * kThreads + tid];
       }
     }
 #pragma unroll
     for (int k = 0; k < U; ++k)
       if (inside >> k & 1u) out[k * kThreads] = x[k];
     out += a.V;
-#pragma unroll
-    for (int k = 0; k < U; ++k) x[k] = next[k];
-    on = next_on;
+    __syncwarp();                       // (the words of this row have been read)
+    get_words(i + 2 * kAhead);
+    get_row(i + kAhead);
+    copies_commit();
   }
 }
 
@@ -183,11 +248,14 @@ LASER_API laser_status laser_adjust_logits(const float* logits, const int32_t* t
   if (B == 0) return LASER_OK;
   AdjustArgs a{logits, out, tokens, parents, n_rows, hist, hist_len, prompt_len, hist_stride, repetition, frequency, presence,
                bias_offsets, bias_ids, bias_values, allowed, mask_seq_stride, mask_row_stride, rows, V};
+  auto launch = [&](auto kernel, int run, int smem) -> laser_status {
+    LASER_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    LASER_CUDA(launch_overlapped(kernel, dim3(unsigned(ceil_div(V, run)), unsigned(B)), kThreads, size_t(smem), as_stream(stream), a));
+    return LASER_OK;
+  };
   // runs of 2048 tokens; of 512 where the SMs would be left without work
-  if (int64_t(B) * ceil_div(V, 8 * kThreads) >= 148)
-    LASER_CUDA(launch_overlapped(adjust_kernel<8>, dim3(unsigned(ceil_div(V, 8 * kThreads)), unsigned(B)), kThreads, 0, as_stream(stream), a));
-  else
-    LASER_CUDA(launch_overlapped(adjust_kernel<2>, dim3(unsigned(ceil_div(V, 2 * kThreads)), unsigned(B)), kThreads, 0, as_stream(stream), a));
+  if (int64_t(B) * ceil_div(V, 8 * kThreads) >= 148) LASER_TRY(launch(adjust_kernel<8>, 8 * kThreads, int(sizeof(Tables<8>))));
+  else LASER_TRY(launch(adjust_kernel<2>, 2 * kThreads, int(sizeof(Tables<2>))));
   count_launch();
   return LASER_OK;
 }
