@@ -18,17 +18,12 @@
 #include <cmath>
 #include <type_traits>
 
-#include "int4.cuh"
-#include "mma.cuh"
-#include "model.cuh"
-#include "tma.cuh"
-#include "tree.cuh"
+#include "attn_int4.cuh"
 
 namespace laser {
 namespace {
 
 using bf16 = __nv_bfloat16;
-constexpr int kMaxSeqs = 1024;     // sequences (or prompt chunks) of a call: their offsets are in shared memory
 constexpr int kMinPages = 2;       // least pages of a warp: two are in flight together anyway
 constexpr int kMostTiles = 5;      // of eight rows in a tile: O takes 160 registers then
 
@@ -53,48 +48,10 @@ struct Sizes {
   static size_t part_floats(int ctas) { return size_t(ctas) * (kWarps * (kOBytes / 4) + 2 * kRecord); }
 };
 
-struct AttnArgs {
-  // rows: from a step's tables (row_ctx, row_n) or the sequences' lengths; parents: a token tree's (up to 64 rows)
-  const int32_t *seq_ids, *row_ctx, *row_n, *n_rows, *seq_len, *parents;
-  int B, Rs, max_seqs, capacity, Hkv, G;       // G: query heads of a kv head
-  const int32_t* page_table;
-  int pages_per_seq;
-  const uint8_t* pages;                        // this layer's
-  const bf16* q;
-  bf16* out;
-  long long ldq, ldo;                          // elements between rows
-  int vec_out;                                 // rows of out are 16-byte aligned
-  unsigned group_inv;                          // 2^32 / G rounded up (G > 1)
-  float scale;                                 // log2(e) / sqrt(dh)
-  float *part;
-  int32_t *arrived, *status;
-};
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-// two codes at bits 3 .. 6 of the halves -> the two values.  (w & 0x00780078) | 0x41804180 as one instruction: of two constants the
-// compiler makes two, and the kernel's busiest pipe is the one for logic and shifts.
-__device__ __forceinline__ uint32_t values(uint32_t w, uint32_t s2, uint32_t z2) {
-  uint32_t u;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(u) : "r"(w), "r"(0x00780078u), "r"(0x41804180u));
-  return fma2(u, s2, z2);
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
-}
-__device__ __forceinline__ void copy_block(uint32_t dst, const void* src, int bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -116,7 +73,6 @@ struct Segment { int b, hk, row0, start, pages; };
 // one that is cut: the warps whose pieces are this CTA's; whether the last of them went on behind it; whether other CTAs have pieces, and
 // then whether they have its beginning
 struct Cut { Segment seg; int first, last; bool early, open, begun; };
-constexpr float kNothing = 1e30f;      // -m of rows that have seen nothing
 
 template <int DH, int NT>
 __global__ void __launch_bounds__(Sizes<DH, NT>::kWarps * 32, 1)
@@ -675,6 +631,11 @@ laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t strea
   a.scale = float(1.4426950408889634 / std::sqrt(double(kv->head_dim)));
   a.group_inv = unsigned(((uint64_t(1) << 32) + a.G - 1) / a.G);
   a.part = kv->attn_part; a.arrived = kv->attn_arrived;
+  if (kv->head_dim == 128) {
+    LASER_TRY(attn_int4_wide_launch(a, kv->attn_ctas, stream));
+    count_launch();
+    return LASER_OK;
+  }
   const int64_t rows = int64_t(a.Rs) * a.G;
   const int nt = row_tiles(int(std::min<int64_t>(rows, 1 << 28)));
   const int64_t units = a.Hkv * ceil_div(rows, int64_t(8 * nt));          // of a sequence, at most
@@ -701,18 +662,18 @@ laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t strea
       default: return launch(attn_int4_kernel<D, 5>, Sizes<D, 5>{});
     }
   };
-  LASER_TRY(kv->head_dim == 128 ? by_tiles(std::integral_constant<int, 128>{}) : by_tiles(std::integral_constant<int, 64>{}));
+  LASER_TRY(by_tiles(std::integral_constant<int, 64>{}));
   count_launch();
   return LASER_OK;
 }
 
 }  // namespace
 
-int attention_int4_max_groups() { return kMaxSeqs; }
+int attention_int4_max_groups() { return kAttnInt4Seqs; }
 size_t attention_int4_part_floats(int head_dim, int ctas) {
+  if (head_dim == 128) return attn_int4_wide_part_floats(ctas);
   auto most = [&](auto... z) { return std::max({decltype(z)::part_floats(ctas)...}); };
-  return head_dim == 128 ? most(Sizes<128, 1>{}, Sizes<128, 2>{}, Sizes<128, 3>{}, Sizes<128, 4>{}, Sizes<128, 5>{})
-                         : most(Sizes<64, 1>{}, Sizes<64, 2>{}, Sizes<64, 3>{}, Sizes<64, 4>{}, Sizes<64, 5>{});
+  return most(Sizes<64, 1>{}, Sizes<64, 2>{}, Sizes<64, 3>{}, Sizes<64, 4>{}, Sizes<64, 5>{});
 }
 
 laser_status attention_int4_launch(laser_model* m, laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* parents, int B, int Rs,
@@ -737,7 +698,7 @@ LASER_API laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int3
   LASER_REQUIRE(kv->pages4, "the cache is not a 4-bit one");
   LASER_REQUIRE(layer >= 0 && layer < kv->n_layers, "layer %d out of range", layer);
   LASER_REQUIRE(B >= 0 && rows >= 1 && int64_t(B) * rows <= INT32_MAX, "B = %d sequences of %d rows", B, rows);
-  if (B > kMaxSeqs) { set_error("B = %d sequences in one call (at most %d)", B, kMaxSeqs); return LASER_ERR_CAPACITY; }
+  if (B > kAttnInt4Seqs) { set_error("B = %d sequences in one call (at most %d)", B, kAttnInt4Seqs); return LASER_ERR_CAPACITY; }
   LASER_REQUIRE(!parents || rows <= 64, "a token tree has at most 64 rows (rows = %d)", rows);
   const int64_t width = int64_t(kv->n_heads) * kv->head_dim;
   LASER_REQUIRE(q_stride >= width && out_stride >= width, "rows overlap: strides %lld, %lld", (long long)q_stride, (long long)out_stride);

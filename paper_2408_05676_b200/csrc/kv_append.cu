@@ -60,7 +60,7 @@ kv_append_kernel(const AppendArgs a) {
   constexpr int LPH = DH / 4, HPW = 32 / LPH;       // lanes of a head, heads of a warp
   constexpr int W = kAppendThreads / 32;
   __shared__ float2 s_cs[kRowsMost][DH / 2];
-  __shared__ int s_par[64], s_pos[kRowsMost];       // a row's position
+  __shared__ int s_pos[kRowsMost];                  // a row's position
   __shared__ void* s_dst[kRowsMost];          // its page (null: the row is not one)
   __shared__ int s_slot[kRowsMost];                 // its place in the page
   next_may_launch();
