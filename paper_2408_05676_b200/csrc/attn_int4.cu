@@ -12,20 +12,28 @@
 // row's result does not depend on where its walk was cut but for the order of fp32 sums.  It is raised only when a score exceeds it by
 // more than 2^6, which a vote finds; p stays below 2^7, and bf16's and fp32's range is left to what is far below.
 //
-// Where a unit is cut, the pieces (m, sum, O in fp32) meet twice: the warps' in their CTA after its last page, the CTAs' in whichever of
-// them arrives last, in the order of the pages both times.  Nothing waits for another CTA.
+// Where a unit is cut, the pieces (m, sum, O in fp32) meet twice, in the order of the pages both times: the warps' in their CTA after its
+// last page, the CTAs' in a kernel that follows.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
 
-#include "attn_int4.cuh"
+#include "int4.cuh"
+#include "mma.cuh"
+#include "model.cuh"
+#include "tma.cuh"
+#include "tree.cuh"
 
 namespace laser {
 namespace {
 
 using bf16 = __nv_bfloat16;
+constexpr int kMaxSeqs = 1024;     // sequences (or prompt chunks) of a call: their offsets are in shared memory
 constexpr int kMinPages = 2;       // least pages of a warp: two are in flight together anyway
 constexpr int kMostTiles = 5;      // of eight rows in a tile: O takes 160 registers then
+
+// a unit that several CTAs have pieces of (count = 0: none)
+struct Join { int b, hk, row0, rows, count; };
 
 template <int DH, int NT>
 struct Sizes {
@@ -41,17 +49,57 @@ struct Sizes {
   static constexpr int kOBytes = kSlices * 512;          // O of a piece
   // A warp's memory: its ring and Q; when those are done with, O of the piece that it ends with and slices of others' first pieces
   static constexpr int kLoop = kStages * kBlock + kQBytes;
-  static constexpr int kRegion = kLoop > kOBytes ? kLoop : kOBytes;
-  static constexpr int kFetched = (kRegion - kOBytes) / 512;
+  static constexpr int kFetched = NT >= 4 ? 8 : 16;
+  static constexpr int kRegion = kLoop > kOBytes + kFetched * 512 ? kLoop : kOBytes + kFetched * 512;
   static constexpr int kRecord = kOBytes / 4 + 16 * NT;  // floats of a CTA's piece: O, then (m, sum) of the rows
   static constexpr int smem(int B) { return kWarps * (kRegion + kStages * 8) + (B + 1) * 8 + B * 12; }
-  static size_t part_floats(int ctas) { return size_t(ctas) * (kWarps * (kOBytes / 4) + 2 * kRecord); }
+  static constexpr int kPart = kWarps * (kOBytes / 4);   // floats of a CTA's warps' first pieces
+  static size_t part_floats(int ctas) { return size_t(ctas) * (kPart + 2 * kRecord) + size_t(ctas) * (sizeof(Join) / 4); }
 };
 
+struct AttnArgs {
+  // rows: from a step's tables (row_ctx, row_n) or the sequences' lengths; parents: a token tree's (up to 64 rows)
+  const int32_t *seq_ids, *row_ctx, *row_n, *n_rows, *seq_len, *parents;
+  int B, Rs, max_seqs, capacity, Hkv, G;       // G: query heads of a kv head
+  const int32_t* page_table;
+  int pages_per_seq;
+  const uint8_t* pages;                        // this layer's
+  const bf16* q;
+  bf16* out;
+  long long ldq, ldo;                          // elements between rows
+  int vec_out;                                 // rows of out are 16-byte aligned
+  unsigned group_inv;                          // 2^32 / G rounded up (G > 1)
+  float scale;                                 // log2(e) / sqrt(dh)
+  float *part, *records;                       // warps' first pieces; CTAs' pieces [CTA][2]: of the unit that it goes on with, that goes on behind it
+  Join* joins;                                 // [CTA] the latter
+  int32_t* status;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+// two codes at bits 3 .. 6 of the halves -> the two values.  (w & 0x00780078) | 0x41804180 as one instruction: of two constants the
+// compiler makes two, and the kernel's busiest pipe is the one for logic and shifts.
+__device__ __forceinline__ uint32_t values(uint32_t w, uint32_t s2, uint32_t z2) {
+  uint32_t u;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(u) : "r"(w), "r"(0x00780078u), "r"(0x41804180u));
+  return fma2(u, s2, z2);
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
+}
+__device__ __forceinline__ void copy_block(uint32_t dst, const void* src, int bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -73,6 +121,7 @@ struct Segment { int b, hk, row0, start, pages; };
 // one that is cut: the warps whose pieces are this CTA's; whether the last of them went on behind it; whether other CTAs have pieces, and
 // then whether they have its beginning
 struct Cut { Segment seg; int first, last; bool early, open, begun; };
+constexpr float kNothing = 1e30f;      // -m of rows that have seen nothing
 
 template <int DH, int NT>
 __global__ void __launch_bounds__(Sizes<DH, NT>::kWarps * 32, 1)
@@ -93,8 +142,8 @@ attn_int4_kernel(const AttnArgs a) {
   __shared__ unsigned long long s_path[W][64];      // token trees: the rows that a row of the warp's sequence sees
   __shared__ Segment s_seg[W][2];                   // the units of a warp's first and of its last page
   __shared__ Cut s_cut[2 * W];
-  __shared__ float2 s_ml[W][2][TM];                 // m and sum of the rows of the piece that a warp began with, if it went on; that it ended with
-  __shared__ int s_abort, s_cuts, s_last[2];
+  __shared__ __align__(16) float2 s_ml[W][2][TM];                 // m and sum of the rows of the piece that a warp began with, if it went on; that it ended with
+  __shared__ int s_abort, s_cuts;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3;
   // a row is verify row row / G, head row % G of its kv head
   auto verify_row = [&](int row) { return a.G == 1 ? row : int(__umulhi(unsigned(row), a.group_inv)); };
@@ -155,12 +204,12 @@ attn_int4_kernel(const AttnArgs a) {
   // (a CTA's share is below 2^31 pages: the cache has no more than that, and a call no more tiles than that allows)
   const int per_cta = max(total <= 0xffffffffll ? int((unsigned(total) + gridDim.x - 1) / gridDim.x) : int((total + gridDim.x - 1) / gridDim.x), 2 * kMinPages);
   const long long c0 = (long long)per_cta * blockIdx.x;
+  if (tid == 0) a.joins[blockIdx.x].count = 0;
   if (c0 >= total) return;
   const int span = int(min(total - c0, (long long)per_cta));      // this CTA's pages
   const int per_warp = max((per_cta + W - 1) / W, kMinPages);
   const int n = min(span - per_warp * warp, per_warp);            // this warp's (none, if that is negative)
 
-  float* const all_part = a.part + size_t(gridDim.x) * W * (Z::kOBytes / 4);                   // [CTA][2] records: CTAs' pieces
   float4* const my_part = reinterpret_cast<float4*>(a.part) + size_t(blockIdx.x * W + warp) * (Z::kSlices * 32) + lane;   // the warp's first piece
 
   if (n > 0) {
@@ -443,8 +492,7 @@ attn_int4_kernel(const AttnArgs a) {
     return;
   }
 
-  // ---- pieces.  Under load a trip to L2 takes 1.5 us, so they stay in shared memory or come there together.  First those of this CTA:
-  // units around its ends and around the places where one warp follows another ----
+  // ---- this CTA's pieces: of units around its ends and around the places where one warp follows another ----
   if (warp == 0) {
     const int w = lane >> 1, begin_w = w * per_warp;
     Cut c{};
@@ -466,154 +514,137 @@ attn_int4_kernel(const AttnArgs a) {
   }
   __syncthreads();
   const int cuts = s_cuts;
-  // a warp's slice x of cut c; a first piece's slices come from L2, the first few of a warp's all at once
-  auto slices = [&](auto&& each) {
-    int turn = 0, fetched = 0;
+  // The slices are the warps' in turn.  Those of first pieces come from L2, as many at a time as there is room for.
+  const int mine = (cuts * Z::kSlices - warp + W - 1) / W;
+  auto tile_rows = [&](const Segment& seg) { return min((s_nr[seg.b] * a.G - seg.row0 + 7) / 8, NT); };      // groups of eight rows that there are
+  float4* const fetched = reinterpret_cast<float4*>(smem + warp * Z::kRegion + Z::kOBytes) + lane;
+  auto fetch = [&](int x0) {
 #pragma unroll 1
-    for (int c = 0; c < cuts; ++c) {
-      int sl = warp - turn;
-      if (sl < 0) sl += W;
-      turn = (turn + Z::kSlices) % W;
-      const int rows8 = min((s_nr[s_cut[c].seg.b] * a.G - s_cut[c].seg.row0 + 7) / 8, NT);
-#pragma unroll 1
-      for (; sl < rows8 * MT; sl += W) {
-        each(s_cut[c], sl, fetched);
-        fetched += s_cut[c].early;
-      }
+    for (int x = x0; x < min(x0 + Z::kFetched, mine); ++x) {
+      const int c = (warp + x * W) / Z::kSlices, sl = warp + x * W - c * Z::kSlices;
+      if (s_cut[c].early)
+        copy16(smem_u32(fetched + (x - x0) * 32), reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * W + s_cut[c].last) * Z::kSlices + sl) * 32 + lane);
     }
   };
-  const uint32_t fetch_at = smem_u32(smem) + warp * Z::kRegion + Z::kOBytes + lane * 16;
-  slices([&](const Cut& c, int sl, int fetched) {
-    if (c.early && fetched < Z::kFetched)
-      copy16(fetch_at + fetched * 512, reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * W + c.last) * Z::kSlices + sl) * 32 + lane);
-  });
-  copies_done();
-  __syncwarp();
-  slices([&](const Cut& c, int sl, int fetched) {
-    const int t = sl / MT, f = sl % MT;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  fetch(0);
+  // what each piece of a row counts, in the place of its m; of a unit that other CTAs have pieces of, m and the sum go with this one's
+  auto record = [&](const Cut& c) { return a.records + size_t(2 * blockIdx.x + (c.begun ? 0 : 1)) * Z::kRecord; };
 #pragma unroll 1
+  for (int y = tid; y < cuts * TM; y += W * 32) {
+    const Cut& c = s_cut[y / TM];
+    const int row = y % TM;
+    float m = -INFINITY, l = 0.f;
+    for (int x = c.first; x <= c.last; ++x) m = fmaxf(m, s_ml[x][c.early && x == c.last ? 0 : 1][row].x);
+    const float zero = m == -INFINITY ? 0.f : m;
     for (int x = c.first; x <= c.last; ++x) {
-      const bool early = c.early && x == c.last;
-      float4 v;
-      if (!early) v = reinterpret_cast<const float4*>(smem + x * Z::kRegion)[sl * 32 + lane];
-      else if (fetched < Z::kFetched) v = reinterpret_cast<const float4*>(smem + warp * Z::kRegion + Z::kOBytes)[fetched * 32 + lane];
-      else v = __ldcg(reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * W + x) * Z::kSlices + sl) * 32 + lane);
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const float2 ml = s_ml[x][early ? 0 : 1][8 * t + 2 * qd + y];
-        const float next = fmaxf(m[y], ml.x), zero = next == -INFINITY ? 0.f : next;
-        const float old = ex2(m[y] - zero), now = ex2(ml.x - zero);
-        m[y] = next;
-        l[y] = l[y] * old + ml.y * now;
-        acc[y] = acc[y] * old + (y ? v.y : v.x) * now;
-        acc[2 + y] = acc[2 + y] * old + (y ? v.w : v.z) * now;
-      }
+      float2& ml = s_ml[x][c.early && x == c.last ? 0 : 1][row];
+      ml.x = ex2(ml.x - zero);
+      l += ml.y * ml.x;
     }
     if (c.open) {
-      float* rec = all_part + size_t(2 * blockIdx.x + (c.begun ? 0 : 1)) * Z::kRecord;
-      __stcg(reinterpret_cast<float4*>(rec) + sl * 32 + lane, make_float4(acc[0], acc[1], acc[2], acc[3]));
-      if (f == 0 && g == 0) __stcg(reinterpret_cast<float4*>(rec + Z::kOBytes / 4) + 4 * t + qd, make_float4(m[0], l[0], m[1], l[1]));
+      __stcg(reinterpret_cast<float2*>(record(c) + Z::kOBytes / 4) + row, make_float2(m, l));
     } else {
-      const int nrows = s_nr[c.seg.b] * a.G;
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int row = c.seg.row0 + 8 * t + 2 * qd + y;
-        if (row >= nrows) continue;
-        const float inv = 1.f / l[y];
-        const int i = verify_row(row), j = row - i * a.G;
-        *reinterpret_cast<uint32_t*>(a.out + (size_t(c.seg.b) * a.Rs + i) * a.ldo + size_t(c.seg.hk * a.G + j) * DH + CPG * g + 2 * f) =
-            pack_bf16(acc[y] * inv, acc[2 + y] * inv);
-      }
+      const float inv = 1.f / l;
+      for (int x = c.first; x <= c.last; ++x) s_ml[x][c.early && x == c.last ? 0 : 1][row].x *= inv;
     }
-  });
-  // the cuts of open units: the first, if the unit began before this CTA, and the last, if it goes on behind it
-  const int open0 = cuts > 0 && s_cut[0].open && s_cut[0].begun ? 0 : -1;
-  const int open1 = cuts > 0 && s_cut[cuts - 1].open && !s_cut[cuts - 1].begun ? cuts - 1 : -1;
-  if (open0 < 0 && open1 < 0) return;
-  __syncthreads();
-  // ---- then, of units that other CTAs have pieces of, those whose last CTA this is ----
-  if (tid < 2) {
-    const int open = tid ? open1 : open0;
-    int last = 0;
-    if (open >= 0) {
-      const Segment& seg = s_cut[open].seg;
-      const int before = seg.start < 0 ? (per_cta - 1 - seg.start) / per_cta : 0, after = (seg.start + seg.pages - 1) / per_cta;     // the unit's other CTAs
-      __threadfence();
-      last = atomicAdd(a.arrived + blockIdx.x - before, 1) == before + after;
-      __threadfence();
-      if (last) a.arrived[blockIdx.x - before] = 0;
-    }
-    s_last[tid] = last;
   }
   __syncthreads();
-  constexpr int kPer = (Z::kSlices + W - 1) / W;      // slices of a warp
 #pragma unroll 1
-  for (int k = 0; k < 2; ++k) {
-    if (!s_last[k]) continue;
-    const Segment seg = s_cut[k ? open1 : open0].seg;
-    const int before = seg.start < 0 ? (per_cta - 1 - seg.start) / per_cta : 0, count = before + (seg.start + seg.pages - 1) / per_cta + 1;
-    // the first CTA's second record, then the others' first ones
-    auto record = [&](int r) { return all_part + (2 * size_t(blockIdx.x - before + r) + (r == 0 ? 1 : 0)) * Z::kRecord; };
-    const int row0 = seg.row0, nrows = s_nr[seg.b] * a.G;
-    const int rows8 = min((nrows - row0 + 7) / 8, NT);                        // groups of eight rows that there are
-    float2* const weight = reinterpret_cast<float2*>(smem);                   // [pieces][rows] (m, sum), then (weight, -); behind them O of pieces
-    const int begin = (count * TM * 8 + 127) & ~127, room = (W * Z::kRegion - begin) / Z::kOBytes;
-    float acc[kPer][4];
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) acc[x][0] = acc[x][1] = acc[x][2] = acc[x][3] = 0.f;
+  for (int x0 = 0; x0 < mine; x0 += Z::kFetched) {
+    if (x0) { __syncwarp(); fetch(x0); }
+    copies_done();                                // (a lane reads what it fetched itself)
 #pragma unroll 1
-    for (int r0 = 0; r0 < count; r0 += room) {
-      const int here = min(room, count - r0);
-      __syncthreads();                      // (what was there before has been read)
-#pragma unroll 1
-      for (int r = 0; r < here; ++r) {
-        const float4* src = reinterpret_cast<const float4*>(record(r0 + r));
-#pragma unroll 1
-        for (int x = tid; x < rows8 * MT * 32; x += W * 32) copy16(smem_u32(smem) + begin + r * Z::kOBytes + x * 16, src + x);
-      }
-      if (r0 == 0) {
-#pragma unroll 1
-        for (int x = tid; x < count * TM; x += W * 32)
-          if (x % TM < 8 * rows8) weight[x] = __ldcg(reinterpret_cast<const float2*>(record(x / TM) + Z::kOBytes / 4) + x % TM);
-        __syncthreads();
-#pragma unroll 1
-        for (int row = warp; row < 8 * rows8; row += W) {
-          float top = -INFINITY, sum = 0.f;
-          for (int r = lane; r < count; r += 32) top = fmaxf(top, weight[r * TM + row].x);
-          for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-          for (int r = lane; r < count; r += 32) sum += weight[r * TM + row].y * ex2(weight[r * TM + row].x - top);
-          for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-          for (int r = lane; r < count; r += 32) weight[r * TM + row].x = ex2(weight[r * TM + row].x - top) / sum;
-        }
-      }
-      copies_done();
-      __syncthreads();
-#pragma unroll
-      for (int x = 0; x < kPer; ++x) {
-        const int sl = warp + x * W, t = sl / MT;
-        if (t >= rows8 || sl >= Z::kSlices) break;
-        const float4* src = reinterpret_cast<const float4*>(smem + begin) + sl * 32 + lane;
+    for (int x = x0; x < min(x0 + Z::kFetched, mine); ++x) {
+      const int at = (warp + x * W) / Z::kSlices, sl = warp + x * W - at * Z::kSlices, t = sl / MT, f = sl % MT;
+      const Cut& c = s_cut[at];
+      if (t >= tile_rows(c.seg)) continue;
+      float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      const int whole = c.early ? c.last : c.last + 1;
+      const float4* o = reinterpret_cast<const float4*>(smem + c.first * Z::kRegion) + sl * 32 + lane;
+      const float4* w = reinterpret_cast<const float4*>(&s_ml[c.first][1][8 * t + 2 * qd]);
+      auto add = [&](const float4& u, const float4& by) {
+        acc[0] += u.x * by.x; acc[1] += u.y * by.z; acc[2] += u.z * by.x; acc[3] += u.w * by.z;
+      };
 #pragma unroll 2
-        for (int r = 0; r < here; ++r) {
-          const float4 v = src[r * (Z::kOBytes / 16)];
-          const float w0 = weight[(r0 + r) * TM + 8 * t + 2 * qd].x, w1 = weight[(r0 + r) * TM + 8 * t + 2 * qd + 1].x;
-          acc[x][0] += v.x * w0; acc[x][1] += v.y * w1; acc[x][2] += v.z * w0; acc[x][3] += v.w * w1;
+      for (int y = c.first; y < whole; ++y, o += Z::kRegion / 16, w += TM) add(*o, *w);
+      if (c.early) add(fetched[(x - x0) * 32], *reinterpret_cast<const float4*>(&s_ml[c.last][0][8 * t + 2 * qd]));
+      if (c.open) {
+        __stcg(reinterpret_cast<float4*>(record(c)) + sl * 32 + lane, make_float4(acc[0], acc[1], acc[2], acc[3]));
+      } else {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int row = c.seg.row0 + 8 * t + 2 * qd + y;
+          if (row >= s_nr[c.seg.b] * a.G) continue;
+          const int i = verify_row(row), j = row - i * a.G;
+          *reinterpret_cast<uint32_t*>(a.out + (size_t(c.seg.b) * a.Rs + i) * a.ldo + size_t(c.seg.hk * a.G + j) * DH + CPG * g + 2 * f) =
+              pack_bf16(acc[y], acc[2 + y]);
         }
       }
     }
+  }
+  // the unit that goes on behind this CTA
+  if (tid == 0 && cuts > 0 && s_cut[cuts - 1].open && !s_cut[cuts - 1].begun) {
+    const Segment& seg = s_cut[cuts - 1].seg;
+    a.joins[blockIdx.x] = Join{seg.b, seg.hk, seg.row0, s_nr[seg.b] * a.G, (seg.start + seg.pages - 1) / per_cta + 1};
+  }
+}
+
+// The units that several CTAs have pieces of: a block a CTA that has a unit's first piece, and eight rows; a warp 16 features.  In a kernel of
+// its own, with a unit's slices over many SMs: the last of its CTAs to arrive, joining alone, took 25 us of 90 where eight units of 40 rows
+// were in 19 pieces each, and still 2 to 5 where they were in 2 or 3; this one takes XX.
+template <int DH, int NT>
+__global__ void __launch_bounds__(DH * 2)
+attn_int4_join_kernel(const AttnArgs a) {
+  using Z = Sizes<DH, NT>;
+  constexpr int MT = DH / 16, kBatch = 12;
+  extern __shared__ __align__(128) uint8_t smem[];
+  float2* const weight = reinterpret_cast<float2*>(smem);      // [pieces][rows] (m, sum), then (weight, -)
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3, t = blockIdx.y;
+  next_may_launch();
+  wait_for_earlier();
+  const Join x = a.joins[blockIdx.x];
+  if (x.count == 0 || x.row0 + 8 * t >= x.rows) return;
+  // the first CTA's second record, then the others' first ones
+  auto record = [&](int r) { return a.records + (2 * size_t(blockIdx.x + r) + (r == 0 ? 1 : 0)) * Z::kRecord; };
+  float4 v[kBatch];
+  auto fetch = [&](int r0) {
 #pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const int sl = warp + x * W, t = sl / MT, c = sl % MT;
-      if (t >= rows8 || sl >= Z::kSlices) break;
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int row = row0 + 8 * t + 2 * qd + y;
-        if (row >= nrows) continue;
-        const int i = verify_row(row), j = row - i * a.G;
-        *reinterpret_cast<uint32_t*>(a.out + (size_t(seg.b) * a.Rs + i) * a.ldo + size_t(seg.hk * a.G + j) * DH + CPG * g + 2 * c) = pack_bf16(acc[x][y], acc[x][2 + y]);
-      }
+    for (int u = 0; u < kBatch; ++u)
+      if (r0 + u < x.count) v[u] = __ldcg(reinterpret_cast<const float4*>(record(r0 + u)) + (t * MT + warp) * 32 + lane);
+  };
+  fetch(0);
+#pragma unroll 1
+  for (int row = warp; row < 8; row += MT) {
+    float top = -INFINITY, sum = 0.f;
+    for (int r = lane; r < x.count; r += 32) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(record(r) + Z::kOBytes / 4) + 8 * t + row);
+      weight[r * 8 + row] = ml;
+      top = fmaxf(top, ml.x);
     }
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    for (int r = lane; r < x.count; r += 32) sum += weight[r * 8 + row].y * ex2(weight[r * 8 + row].x - top);
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    const float inv = 1.f / sum;      // (a row sees itself: its sum is not zero)
+    for (int r = lane; r < x.count; r += 32) weight[r * 8 + row].x = ex2(weight[r * 8 + row].x - top) * inv;
+  }
+  __syncthreads();
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int r0 = 0; r0 < x.count; r0 += kBatch) {
+    if (r0) fetch(r0);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (r0 + u >= x.count) break;
+      const float4 w = *reinterpret_cast<const float4*>(&weight[(r0 + u) * 8 + 2 * qd]);
+      acc[0] += v[u].x * w.x; acc[1] += v[u].y * w.z; acc[2] += v[u].z * w.x; acc[3] += v[u].w * w.z;
+    }
+  }
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const int row = x.row0 + 8 * t + 2 * qd + y;
+    if (row >= x.rows) continue;
+    const int i = a.G == 1 ? row : int(__umulhi(unsigned(row), a.group_inv)), j = row - i * a.G;
+    *reinterpret_cast<uint32_t*>(a.out + (size_t(x.b) * a.Rs + i) * a.ldo + size_t(x.hk * a.G + j) * DH + MT * 2 * g + 2 * warp) = pack_bf16(acc[y], acc[2 + y]);
   }
 }
 
@@ -630,12 +661,7 @@ laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t strea
   a.page_table = kv->page_table; a.pages_per_seq = kv->pages_per_seq;
   a.scale = float(1.4426950408889634 / std::sqrt(double(kv->head_dim)));
   a.group_inv = unsigned(((uint64_t(1) << 32) + a.G - 1) / a.G);
-  a.part = kv->attn_part; a.arrived = kv->attn_arrived;
-  if (kv->head_dim == 128) {
-    LASER_TRY(attn_int4_wide_launch(a, kv->attn_ctas, stream));
-    count_launch();
-    return LASER_OK;
-  }
+  a.part = kv->attn_part;
   const int64_t rows = int64_t(a.Rs) * a.G;
   const int nt = row_tiles(int(std::min<int64_t>(rows, 1 << 28)));
   const int64_t units = a.Hkv * ceil_div(rows, int64_t(8 * nt));          // of a sequence, at most
@@ -644,36 +670,42 @@ laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t strea
     return LASER_ERR_CAPACITY;
   }
   a.vec_out = (reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo * 2)) % 16 == 0;
-  auto launch = [&](auto kernel, auto sizes) -> laser_status {
+  auto launch = [&](auto kernel, auto join, auto sizes) -> laser_status {
     using Z = decltype(sizes);
     const int smem = Z::smem(a.B);
     const unsigned grid = unsigned(std::min<int64_t>(kv->attn_ctas, units * a.B * kv->pages_per_seq));
     LASER_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    a.records = a.part + size_t(grid) * Z::kPart;
+    a.joins = reinterpret_cast<Join*>(a.records + size_t(grid) * 2 * Z::kRecord);
     LASER_CUDA(launch_overlapped(kernel, dim3(grid), Z::kWarps * 32, size_t(smem), stream, a));
+    count_launch();
+    if (grid > 1) {
+      LASER_CUDA(launch_overlapped(join, dim3(grid, nt), kv->head_dim * 2, size_t(grid) * 64, stream, a));
+      count_launch();
+    }
     return LASER_OK;
   };
   auto by_tiles = [&](auto dh) -> laser_status {
     constexpr int D = decltype(dh)::value;
     switch (nt) {
-      case 1: return launch(attn_int4_kernel<D, 1>, Sizes<D, 1>{});
-      case 2: return launch(attn_int4_kernel<D, 2>, Sizes<D, 2>{});
-      case 3: return launch(attn_int4_kernel<D, 3>, Sizes<D, 3>{});
-      case 4: return launch(attn_int4_kernel<D, 4>, Sizes<D, 4>{});
-      default: return launch(attn_int4_kernel<D, 5>, Sizes<D, 5>{});
+      case 1: return launch(attn_int4_kernel<D, 1>, attn_int4_join_kernel<D, 1>, Sizes<D, 1>{});
+      case 2: return launch(attn_int4_kernel<D, 2>, attn_int4_join_kernel<D, 2>, Sizes<D, 2>{});
+      case 3: return launch(attn_int4_kernel<D, 3>, attn_int4_join_kernel<D, 3>, Sizes<D, 3>{});
+      case 4: return launch(attn_int4_kernel<D, 4>, attn_int4_join_kernel<D, 4>, Sizes<D, 4>{});
+      default: return launch(attn_int4_kernel<D, 5>, attn_int4_join_kernel<D, 5>, Sizes<D, 5>{});
     }
   };
-  LASER_TRY(by_tiles(std::integral_constant<int, 64>{}));
-  count_launch();
+  LASER_TRY(kv->head_dim == 128 ? by_tiles(std::integral_constant<int, 128>{}) : by_tiles(std::integral_constant<int, 64>{}));
   return LASER_OK;
 }
 
 }  // namespace
 
-int attention_int4_max_groups() { return kAttnInt4Seqs; }
+int attention_int4_max_groups() { return kMaxSeqs; }
 size_t attention_int4_part_floats(int head_dim, int ctas) {
-  if (head_dim == 128) return attn_int4_wide_part_floats(ctas);
   auto most = [&](auto... z) { return std::max({decltype(z)::part_floats(ctas)...}); };
-  return most(Sizes<64, 1>{}, Sizes<64, 2>{}, Sizes<64, 3>{}, Sizes<64, 4>{}, Sizes<64, 5>{});
+  return head_dim == 128 ? most(Sizes<128, 1>{}, Sizes<128, 2>{}, Sizes<128, 3>{}, Sizes<128, 4>{}, Sizes<128, 5>{})
+                         : most(Sizes<64, 1>{}, Sizes<64, 2>{}, Sizes<64, 3>{}, Sizes<64, 4>{}, Sizes<64, 5>{});
 }
 
 laser_status attention_int4_launch(laser_model* m, laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* parents, int B, int Rs,
@@ -698,7 +730,7 @@ LASER_API laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int3
   LASER_REQUIRE(kv->pages4, "the cache is not a 4-bit one");
   LASER_REQUIRE(layer >= 0 && layer < kv->n_layers, "layer %d out of range", layer);
   LASER_REQUIRE(B >= 0 && rows >= 1 && int64_t(B) * rows <= INT32_MAX, "B = %d sequences of %d rows", B, rows);
-  if (B > kAttnInt4Seqs) { set_error("B = %d sequences in one call (at most %d)", B, kAttnInt4Seqs); return LASER_ERR_CAPACITY; }
+  if (B > kMaxSeqs) { set_error("B = %d sequences in one call (at most %d)", B, kMaxSeqs); return LASER_ERR_CAPACITY; }
   LASER_REQUIRE(!parents || rows <= 64, "a token tree has at most 64 rows (rows = %d)", rows);
   const int64_t width = int64_t(kv->n_heads) * kv->head_dim;
   LASER_REQUIRE(q_stride >= width && out_stride >= width, "rows overlap: strides %lld, %lld", (long long)q_stride, (long long)out_stride);

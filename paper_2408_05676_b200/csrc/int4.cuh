@@ -4,20 +4,13 @@
 // as bf16, so that two codes become two values by one logic instruction and one packed multiply-add.  Everything held is finite: NaN is
 // stored as 0 and magnitudes above 2^124 as 2^124, so that a masked token cannot spoil a row (weight 0 times its value is 0).
 //
-// A page and kv head is one block of 20 head_dim bytes, a single bulk copy, in the order that the attention kernel of that head size takes it.
-// A word of K codes holds features 8i .. 8i + 7 of a token, feature c at bits 3 + 4 (c / 2) + 16 (c % 2) on (mod 32): rotating right by 4e
-// leaves features 2e and 2e + 1 at bits 3 .. 6 of the two halves.  A word of V codes holds features 4j .. 4j + 3 of two tokens, 2u + p at bits
-// 16p + 4e on.
-// head_dim 64 (warp-level MMAs: a lane 4g + q has the fragments of its words)
-//   K codes   [16 tokens][8 words]
-//   K scales  [16 tokens][2]             s | z << 16
-//   V codes   [2][8][4][2 words]         token 8h + 2q + p, features 8g + 4w + e: word [h][g][q][w]
-//   V scales  [2][4][2]                  group, q, h: {s of p = 0, 1}, {z of p = 0, 1}
-// head_dim 128 (tensor memory: a thread unpacks the keys of a token, or the values of a feature)
-//   K codes   [4 groups][16 tokens][4 words]
-//   K scales  [16 tokens][4]             s | z << 16
-//   V codes   [32 features by fours][8 pairs of tokens]
-//   V scales  [4 groups][8 pairs]        {s of p = 0, 1}, {z of p = 0, 1}
+// A page and kv head is one block of 20 head_dim bytes, a single bulk copy:
+//   K codes   [16 tokens][head_dim / 8 words]   word: features 8i .. 8i+7, feature c at bits 3 + 4 (c / 2) + 16 (c % 2) on (mod 32): rotating
+//                                               right by 4e leaves features 2e and 2e+1 at bits 3 .. 6 of the two halves
+//   K scales  [16 tokens][head_dim / 32]        s | z << 16
+//   V codes   [2][8][4][head_dim / 32 words]    token 8h + 2q + p, feature (head_dim / 8) g + 4w + e: word [h][g][q][w], bits 16p + 4e on
+//   V scales  [head_dim / 32][4][2]             group, q, h: {s of p = 0, 1}, {z of p = 0, 1}
+// which are the registers of a warp-level MMA's fragments (lane 4g + q) in the order that one wide load of a lane takes them.
 #pragma once
 #include "state.cuh"
 
@@ -27,17 +20,16 @@ constexpr int kQ4Group = 32;
 constexpr float kQ4Top = 0x1p124f, kQ4Least = 0x1p-100f;
 
 __host__ __device__ constexpr int q4_block_bytes(int dh) { return 20 * dh; }
-__host__ __device__ constexpr int q4_k_codes(int dh, int t, int word) {
-  return dh == 64 ? t * 32 + 4 * word : (word >> 2) * 256 + t * 16 + (word & 3) * 4;
-}
+__host__ __device__ constexpr int q4_k_codes(int dh, int t, int word) { return t * (dh / 2) + 4 * word; }
 __host__ __device__ constexpr int q4_k_scale(int dh, int t, int group) { return 8 * dh + (t * (dh / 32) + group) * 4; }
 // the 16-bit piece of features 4 c4 .. 4 c4 + 3
 __host__ __device__ constexpr int q4_v_codes(int dh, int t, int c4) {
-  return 10 * dh + (t & 1) * 2 + (dh == 64 ? (((t >> 3) * 8 + c4 / 2) * 4 + ((t & 7) >> 1)) * 8 + c4 % 2 * 4 : c4 * 32 + (t >> 1) * 4);
+  const int per = dh / 32, g = c4 / per, w = c4 % per;
+  return 10 * dh + (((t >> 3) * 8 + g) * 4 + ((t & 7) >> 1)) * per * 4 + w * 4 + (t & 1) * 2;
 }
 // s; z is four bytes further
 __host__ __device__ constexpr int q4_v_scale(int dh, int t, int group) {
-  return 18 * dh + (t & 1) * 2 + (dh == 64 ? ((group * 4 + ((t & 7) >> 1)) * 2 + (t >> 3)) * 8 : (group * 8 + (t >> 1)) * 8);
+  return 18 * dh + ((group * 4 + ((t & 7) >> 1)) * 2 + (t >> 3)) * 8 + (t & 1) * 2;
 }
 
 #ifdef __CUDACC__

@@ -60,7 +60,7 @@ kv_append_kernel(const AppendArgs a) {
   constexpr int LPH = DH / 4, HPW = 32 / LPH;       // lanes of a head, heads of a warp
   constexpr int W = kAppendThreads / 32;
   __shared__ float2 s_cs[kRowsMost][DH / 2];
-  __shared__ int s_pos[kRowsMost];                  // a row's position
+  __shared__ int s_par[64], s_pos[kRowsMost];       // a row's position
   __shared__ void* s_dst[kRowsMost];          // its page (null: the row is not one)
   __shared__ int s_slot[kRowsMost];                 // its place in the page
   next_may_launch();
@@ -390,7 +390,6 @@ LASER_API laser_status laser_kv_check(laser_kv* kv, void* stream) {
   LASER_CUDA(cudaStreamSynchronize(as_stream(stream)));
   if (st == 0) return LASER_OK;
   LASER_CUDA(cudaMemsetAsync(kv->status, 0, 4, as_stream(stream)));
-  if (kv->attn_arrived) LASER_CUDA(cudaMemsetAsync(kv->attn_arrived, 0, size_t(kv->attn_ctas) * sizeof(int32_t), as_stream(stream)));
   set_error(st == LASER_ERR_CAPACITY ? "a sequence outgrew its KV pages"
             : st == LASER_ERR_TIMEOUT ? "a device-side wait ran out" : "a call was given a bad sequence id or parent");
   return st;

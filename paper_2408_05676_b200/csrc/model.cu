@@ -413,7 +413,7 @@ LASER_API laser_status laser_model_create(const laser_model_cfg* cfg, const lase
 LASER_API laser_status laser_kv_free(laser_kv* kv) {
   if (!kv) return LASER_OK;
   cudaFree(kv->pages); cudaFree(kv->pages4); cudaFree(kv->page_table); cudaFree(kv->seq_len);
-  cudaFree(kv->inv_freq); cudaFree(kv->status); cudaFree(kv->attn_part); cudaFree(kv->attn_arrived);
+  cudaFree(kv->inv_freq); cudaFree(kv->status); cudaFree(kv->attn_part);
   delete kv;
   return LASER_OK;
 }
@@ -475,8 +475,6 @@ LASER_API laser_status laser_kv_create_int4(laser_model* m, int32_t max_seqs, in
   LASER_CUDA(cudaGetDevice(&dev));
   LASER_CUDA(cudaDeviceGetAttribute(&kv->attn_ctas, cudaDevAttrMultiProcessorCount, dev));
   LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->attn_part), attention_int4_part_floats(kv->head_dim, kv->attn_ctas) * sizeof(float)));
-  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->attn_arrived), size_t(kv->attn_ctas) * sizeof(int32_t)));
-  LASER_CUDA(cudaMemset(kv->attn_arrived, 0, size_t(kv->attn_ctas) * sizeof(int32_t)));
   guard.p = nullptr;
   *out = kv;
   return LASER_OK;
