@@ -514,16 +514,18 @@ attn_int4_kernel(const AttnArgs a) {
   }
   __syncthreads();
   const int cuts = s_cuts;
-  // The slices are the warps' in turn.  Those of first pieces come from L2, as many at a time as there is room for.
-  const int mine = (cuts * Z::kSlices - warp + W - 1) / W;
-  auto tile_rows = [&](const Segment& seg) { return min((s_nr[seg.b] * a.G - seg.row0 + 7) / 8, NT); };      // groups of eight rows that there are
+  // Four slices of eight rows at a time, the warps in turn.  First pieces' come from L2, as many together as there is room for.
+  constexpr int kParts = Z::kSlices / 4, kTogether = Z::kFetched / 4;
+  const int mine = (cuts * kParts - warp + W - 1) / W;
   float4* const fetched = reinterpret_cast<float4*>(smem + warp * Z::kRegion + Z::kOBytes) + lane;
   auto fetch = [&](int x0) {
 #pragma unroll 1
-    for (int x = x0; x < min(x0 + Z::kFetched, mine); ++x) {
-      const int c = (warp + x * W) / Z::kSlices, sl = warp + x * W - c * Z::kSlices;
-      if (s_cut[c].early)
-        copy16(smem_u32(fetched + (x - x0) * 32), reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * W + s_cut[c].last) * Z::kSlices + sl) * 32 + lane);
+    for (int x = x0; x < min(x0 + kTogether, mine); ++x) {
+      const int c = (warp + x * W) / kParts, part = warp + x * W - c * kParts;
+      if (!s_cut[c].early) continue;
+      const float4* from = reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * W + s_cut[c].last) * Z::kSlices + 4 * part) * 32 + lane;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) copy16(smem_u32(fetched + ((x - x0) * 4 + k) * 32), from + k * 32);
     }
   };
   fetch(0);
@@ -550,34 +552,42 @@ attn_int4_kernel(const AttnArgs a) {
   }
   __syncthreads();
 #pragma unroll 1
-  for (int x0 = 0; x0 < mine; x0 += Z::kFetched) {
-    if (x0) { __syncwarp(); fetch(x0); }
+  for (int x0 = 0; x0 < mine; x0 += kTogether) {
+    if (x0) fetch(x0);
     copies_done();                                // (a lane reads what it fetched itself)
 #pragma unroll 1
-    for (int x = x0; x < min(x0 + Z::kFetched, mine); ++x) {
-      const int at = (warp + x * W) / Z::kSlices, sl = warp + x * W - at * Z::kSlices, t = sl / MT, f = sl % MT;
+    for (int x = x0; x < min(x0 + kTogether, mine); ++x) {
+      const int at = (warp + x * W) / kParts, part = warp + x * W - at * kParts, t = part / (MT / 4), f = part % (MT / 4) * 4;
       const Cut& c = s_cut[at];
-      if (t >= tile_rows(c.seg)) continue;
-      float acc[4] = {0.f, 0.f, 0.f, 0.f};
-      const int whole = c.early ? c.last : c.last + 1;
-      const float4* o = reinterpret_cast<const float4*>(smem + c.first * Z::kRegion) + sl * 32 + lane;
-      const float4* w = reinterpret_cast<const float4*>(&s_ml[c.first][1][8 * t + 2 * qd]);
-      auto add = [&](const float4& u, const float4& by) {
-        acc[0] += u.x * by.x; acc[1] += u.y * by.z; acc[2] += u.z * by.x; acc[3] += u.w * by.z;
+      const int first = c.first, last = c.last, nrows = s_nr[c.seg.b] * a.G;
+      const bool early = c.early;
+      if (c.seg.row0 + 8 * t >= nrows) continue;
+      float acc[4][4] = {};
+      const float4* o = reinterpret_cast<const float4*>(smem + first * Z::kRegion) + part * 128 + lane;
+      const float4* w = reinterpret_cast<const float4*>(&s_ml[first][1][8 * t + 2 * qd]);
+      auto add = [&](const float4* from, const float4& by) {
+        float4 u[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] = from[k * 32];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { acc[k][0] += u[k].x * by.x; acc[k][1] += u[k].y * by.z; acc[k][2] += u[k].z * by.x; acc[k][3] += u[k].w * by.z; }
       };
-#pragma unroll 2
-      for (int y = c.first; y < whole; ++y, o += Z::kRegion / 16, w += TM) add(*o, *w);
-      if (c.early) add(fetched[(x - x0) * 32], *reinterpret_cast<const float4*>(&s_ml[c.last][0][8 * t + 2 * qd]));
+#pragma unroll 1
+      for (int y = early ? last - first : last - first + 1; y > 0; --y, o += Z::kRegion / 16, w += TM) add(o, *w);
+      if (early) add(fetched + (x - x0) * 128, *reinterpret_cast<const float4*>(&s_ml[last][0][8 * t + 2 * qd]));
       if (c.open) {
-        __stcg(reinterpret_cast<float4*>(record(c)) + sl * 32 + lane, make_float4(acc[0], acc[1], acc[2], acc[3]));
+        float4* to = reinterpret_cast<float4*>(record(c)) + part * 128 + lane;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) __stcg(to + k * 32, make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]));
       } else {
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const int row = c.seg.row0 + 8 * t + 2 * qd + y;
-          if (row >= s_nr[c.seg.b] * a.G) continue;
+          if (row >= nrows) continue;
           const int i = verify_row(row), j = row - i * a.G;
-          *reinterpret_cast<uint32_t*>(a.out + (size_t(c.seg.b) * a.Rs + i) * a.ldo + size_t(c.seg.hk * a.G + j) * DH + CPG * g + 2 * f) =
-              pack_bf16(acc[y], acc[2 + y]);
+          uint32_t* to = reinterpret_cast<uint32_t*>(a.out + (size_t(c.seg.b) * a.Rs + i) * a.ldo + size_t(c.seg.hk * a.G + j) * DH + CPG * g + 2 * f);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) to[k] = pack_bf16(acc[k][y], acc[k][2 + y]);
         }
       }
     }
