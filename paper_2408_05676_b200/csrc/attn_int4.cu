@@ -29,7 +29,6 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kMaxSeqs = 1024;     // sequences (or prompt chunks) of a call: their offsets are in shared memory
-constexpr int kMinPages = 2;       // least pages of a warp: two are in flight together anyway
 constexpr int kMostTiles = 5;      // of eight rows in a tile: O takes 160 registers then
 
 // a unit that several CTAs have pieces of (count = 0: none)
@@ -37,23 +36,26 @@ struct Join { int b, hk, row0, rows, count; };
 
 template <int DH, int NT>
 struct Sizes {
-  static constexpr int kRegsO = NT * DH / 4;             // O registers of a lane
-  // as many warps as the registers allow without spills
-  static constexpr int kWarps = kRegsO <= 32 ? 16 : kRegsO <= 64 ? 12 : 8;
+  // A team is a warp, or two that take a page each of every two and half of the features each
+  static constexpr int kTeam = NT == 1 ? 1 : 2;
+  static constexpr int kRegsO = NT * DH / 4 / kTeam;     // O registers of a lane
+  static constexpr int kWarps = kRegsO <= 32 ? 16 : kRegsO <= 48 ? 12 : 8;      // as many as the registers allow without spills
+  static constexpr int kTeams = kWarps / kTeam;
   static constexpr int kRows = 8 * NT;
   static constexpr int kBlock = q4_block_bytes(DH);      // bytes of a page and head
-  static constexpr int kStages = DH == 64 ? 6 : 4;
+  static constexpr int kStages = DH == 64 ? 6 : kTeam == 1 ? 4 : 3;      // of a warp's ring
   static constexpr bool kQInSmem = NT > 1;               // each lane's share of Q is put by and read again for every page
   static constexpr int kQBytes = kQInSmem ? NT * DH / 8 * 4 * 32 : 0;
+  static constexpr int kPBytes = kTeam == 1 ? 0 : NT * 2 * 256;          // P of two pages
   static constexpr int kSlices = NT * DH / 16;           // of O: four registers, two neighbouring features of two rows
   static constexpr int kOBytes = kSlices * 512;          // O of a piece
-  // A warp's memory: its ring and Q; when those are done with, O of the piece that it ends with and slices of others' first pieces
-  static constexpr int kLoop = kStages * kBlock + kQBytes;
-  static constexpr int kFetched = NT >= 4 ? 8 : 16;
-  static constexpr int kRegion = kLoop > kOBytes + kFetched * 512 ? kLoop : kOBytes + kFetched * 512;
+  // A team's memory: its rings, Q and P; when those are done with, O of the piece that it ends with and slices of others' first pieces
+  static constexpr int kLoop = kTeam * kStages * kBlock + kQBytes + 2 * kPBytes;
+  static constexpr int kFetched = kTeam == 1 ? 16 : 8;   // slices of a warp
+  static constexpr int kRegion = kLoop > kOBytes + kTeam * kFetched * 512 ? kLoop : kOBytes + kTeam * kFetched * 512;
   static constexpr int kRecord = kOBytes / 4 + 16 * NT;  // floats of a CTA's piece: O, then (m, sum) of the rows
-  static constexpr int smem(int B) { return kWarps * (kRegion + kStages * 8) + (B + 1) * 8 + B * 12; }
-  static constexpr int kPart = kWarps * (kOBytes / 4);   // floats of a CTA's warps' first pieces
+  static constexpr int smem(int B) { return kTeams * kRegion + kWarps * kStages * 8 + (B + 1) * 8 + B * 12; }
+  static constexpr int kPart = kTeams * (kOBytes / 4);   // floats of a CTA's teams' first pieces
   static size_t part_floats(int ctas) { return size_t(ctas) * (kPart + 2 * kRecord) + size_t(ctas) * (sizeof(Join) / 4); }
 };
 
@@ -107,18 +109,29 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void lds(uint32_t (&w)[N], const uint8_t* p) {
-  if (N == 4) {
+  if (N == 1) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if (N == 4) {
     const uint4 u = *reinterpret_cast<const uint4*>(p);
-    w[0] = u.x; w[1] = u.y; w[2 % N] = u.z; w[3 % N] = u.w;
+    w[0] = u.x; w[1 % N] = u.y; w[2 % N] = u.z; w[3 % N] = u.w;
   } else {
     const uint2 u = *reinterpret_cast<const uint2*>(p);
-    w[0] = u.x; w[1] = u.y;
+    w[0] = u.x; w[1 % N] = u.y;
   }
 }
 
-// a unit: its sequence, kv head and first row; its first page (from the CTA's first) and its pages
-struct Segment { int b, hk, row0, start, pages; };
-// one that is cut: the warps whose pieces are this CTA's; whether the last of them went on behind it; whether other CTAs have pieces, and
+// of two warps: all have come here; whether any thread says so
+__device__ __forceinline__ void team_sync(int team) { asm volatile("bar.sync %0, 64;" ::"r"(1 + team) : "memory"); }
+__device__ __forceinline__ bool team_any(int team, bool x) {
+  uint32_t y;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbar.red.or.pred q, %2, 64, p;\nselp.u32 %0, 1, 0, q;\n}"
+               : "=r"(y) : "r"(uint32_t(x)), "r"(1 + team) : "memory");
+  return y != 0;
+}
+
+// a unit: its sequence, kv head and first row; its first block (from the CTA's first) and its blocks
+struct Segment { int b, hk, row0, start, blocks; };
+// one that is cut: the teams whose pieces are this CTA's; whether the last of them went on behind it; whether other CTAs have pieces, and
 // then whether they have its beginning
 struct Cut { Segment seg; int first, last; bool early, open, begun; };
 constexpr float kNothing = 1e30f;      // -m of rows that have seen nothing
@@ -127,24 +140,27 @@ template <int DH, int NT>
 __global__ void __launch_bounds__(Sizes<DH, NT>::kWarps * 32, 1)
 attn_int4_kernel(const AttnArgs a) {
   using Z = Sizes<DH, NT>;
-  constexpr int W = Z::kWarps, ST = Z::kStages, TM = Z::kRows, BLK = Z::kBlock;
+  constexpr int S = Z::kTeam, W = Z::kWarps, T = Z::kTeams, ST = Z::kStages, TM = Z::kRows, BLK = Z::kBlock;
   constexpr int KW = DH / 32;            // words of a lane's K (of a token) or V (of two tokens)
+  constexpr int VW = KW / S;             // of V, a warp's
   constexpr int CPG = DH / 8;            // output features of a lane
   constexpr int MT = DH / 16;            // 16-feature tiles
+  constexpr int OT = MT / S;             // a warp's
   constexpr int QC = DH / 32;            // 16-byte pieces of a lane's share of a Q row
   extern __shared__ __align__(128) uint8_t smem[];
-  uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + W * Z::kRegion);        // [W][ST], behind the warps' regions
-  long long* const s_pre = reinterpret_cast<long long*>(bars + W * ST);             // [B + 1] pages before a sequence
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + T * Z::kRegion);        // [W][ST], behind the teams' regions
+  long long* const s_pre = reinterpret_cast<long long*>(bars + W * ST);             // [B + 1] blocks before a sequence
   int* const s_ctx = reinterpret_cast<int*>(s_pre + a.B + 1);                       // [B]
   int* const s_nr = s_ctx + a.B;                                                    // [B]
   int* const s_seq = s_nr + a.B;                                                    // [B]
   __shared__ long long s_sum[W];
-  __shared__ unsigned long long s_path[W][64];      // token trees: the rows that a row of the warp's sequence sees
-  __shared__ Segment s_seg[W][2];                   // the units of a warp's first and of its last page
-  __shared__ Cut s_cut[2 * W];
-  __shared__ __align__(16) float2 s_ml[W][2][TM];                 // m and sum of the rows of the piece that a warp began with, if it went on; that it ended with
+  __shared__ unsigned long long s_path[T][64];      // token trees: the rows that a row of the team's sequence sees
+  __shared__ Segment s_seg[T][2];                   // the units of a team's first and of its last block
+  __shared__ Cut s_cut[2 * T];
+  __shared__ __align__(16) float2 s_ml[T][2][TM];   // m and sum of the rows of the piece that a team began with, if it went on; that it ended with
+  __shared__ float s_half[S == 1 ? 1 : W][TM];      // what a warp tells the other of its rows: highest scores, or sums
   __shared__ int s_abort, s_cuts;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3, team = warp / S, half = warp % S;
   // a row is verify row row / G, head row % G of its kv head
   auto verify_row = [&](int row) { return a.G == 1 ? row : int(__umulhi(unsigned(row), a.group_inv)); };
 
@@ -157,8 +173,9 @@ attn_int4_kernel(const AttnArgs a) {
   // a step's tables were complete before any kernel of the forward began
   if (!a.row_ctx) wait_for_earlier();
 
-  // ---- the units: pages of all sequences, one after another ----
+  // ---- the units: blocks of S pages of all sequences, one after another ----
   auto tiles_of = [&](int nr) { return (nr * a.G + TM - 1) / TM; };
+  auto pages_of = [&](int b) { return (s_ctx[b] + s_nr[b] + 15) >> 4; };
   long long total = 0;
   for (int b0 = 0; b0 < a.B; b0 += W * 32) {
     const int b = b0 + tid;
@@ -182,7 +199,7 @@ attn_int4_kernel(const AttnArgs a) {
       }
       s_ctx[b] = ctx; s_nr[b] = nr; s_seq[b] = seq;
     }
-    const long long mine = nr > 0 ? (long long)(a.Hkv * tiles_of(nr)) * ((ctx + nr + 15) >> 4) : 0;
+    const long long mine = nr > 0 ? (long long)(a.Hkv * tiles_of(nr)) * ((((ctx + nr + 15) >> 4) + S - 1) / S) : 0;
     long long x = mine;
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, x, o);
@@ -201,37 +218,38 @@ attn_int4_kernel(const AttnArgs a) {
     __syncthreads();
   }
   if (a.row_ctx) wait_for_earlier();
-  // (a CTA's share is below 2^31 pages: the cache has no more than that, and a call no more tiles than that allows)
-  const int per_cta = max(total <= 0xffffffffll ? int((unsigned(total) + gridDim.x - 1) / gridDim.x) : int((total + gridDim.x - 1) / gridDim.x), 2 * kMinPages);
+  // (a CTA's share is below 2^31 blocks: the cache has no more than that, and a call no more tiles than that allows)
+  constexpr int kLeast = 2 / S;        // blocks of a team: two pages are in flight together anyway
+  const int per_cta = max(total <= 0xffffffffll ? int((unsigned(total) + gridDim.x - 1) / gridDim.x) : int((total + gridDim.x - 1) / gridDim.x), 2 * kLeast);
   const long long c0 = (long long)per_cta * blockIdx.x;
   if (tid == 0) a.joins[blockIdx.x].count = 0;
   if (c0 >= total) return;
-  const int span = int(min(total - c0, (long long)per_cta));      // this CTA's pages
-  const int per_warp = max((per_cta + W - 1) / W, kMinPages);
-  const int n = min(span - per_warp * warp, per_warp);            // this warp's (none, if that is negative)
+  const int span = int(min(total - c0, (long long)per_cta));      // this CTA's blocks
+  const int per_team = max((per_cta + T - 1) / T, kLeast);
+  const int n = min(span - per_team * team, per_team);            // this team's (none, if that is negative)
 
-  float4* const my_part = reinterpret_cast<float4*>(a.part) + size_t(blockIdx.x * W + warp) * (Z::kSlices * 32) + lane;   // the warp's first piece
+  float4* const my_part = reinterpret_cast<float4*>(a.part) + size_t(blockIdx.x * T + team) * (Z::kSlices * 32) + lane;   // the team's first piece
 
   if (n > 0) {
-    uint8_t* const my_ring = smem + warp * Z::kRegion;
-    const uint32_t ring_at = smem_u32(my_ring), bar_at = smem_u32(bars + warp * ST);
-    // ---- where the warp begins ----
-    int b, tile, hk, page;
+    uint8_t* const region = smem + team * Z::kRegion;
+    const uint32_t ring_at = smem_u32(region) + half * (ST * BLK), bar_at = smem_u32(bars + warp * ST);
+    // ---- where the team begins ----
+    int b, tile, hk, blk;
     {
-      const long long x = c0 + per_warp * warp;
+      const long long x = c0 + per_team * team;
       int lo = 0, hi = a.B - 1;
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (s_pre[mid] <= x) lo = mid; else hi = mid - 1;
       }
       b = lo;
-      const unsigned at = unsigned(x - s_pre[b]), pg = unsigned(s_ctx[b] + s_nr[b] + 15) >> 4, unit = at / pg, tl = unsigned(tiles_of(s_nr[b]));
-      page = int(at - unit * pg); hk = int(unit / tl); tile = int(unit - hk * tl);
+      const unsigned at = unsigned(x - s_pre[b]), of = unsigned(pages_of(b) + S - 1) / S, unit = at / of, tl = unsigned(tiles_of(s_nr[b]));
+      blk = int(at - unit * of); hk = int(unit / tl); tile = int(unit - hk * tl);
     }
-    int pages = (s_ctx[b] + s_nr[b] + 15) >> 4, tiles = tiles_of(s_nr[b]);
+    int pages = pages_of(b), blocks = (pages + S - 1) / S, tiles = tiles_of(s_nr[b]);
 
-    // ---- copies: a cursor that runs ST pages ahead; of 32 pages each lane holds one's address and requests that page ----
-    int p_b = b, p_tile = tile, p_hk = hk, p_page = page, p_pages = pages, p_tiles = tiles, p_window = -1, p_id = 0;
+    // ---- copies: a cursor that runs ST blocks ahead; of 32 pages each lane holds one's address and requests that page ----
+    int p_b = b, p_tile = tile, p_hk = hk, p_page = blk * S + half, p_pages = pages, p_tiles = tiles, p_window = -1, p_id = 0;
     const uint8_t* p_src = nullptr;
     auto aim = [&]() {
       if (p_window != (p_page & ~31)) {
@@ -242,11 +260,16 @@ attn_int4_kernel(const AttnArgs a) {
     };
     auto request = [&](int s) {
       if (lane == (p_page & 31)) {
-        mbar_expect_tx(bar_at + s * 8, BLK);
-        copy_block(ring_at + s * BLK, p_src, BLK, bar_at + s * 8);
+        if (S == 1 || p_page < p_pages) {
+          mbar_expect_tx(bar_at + s * 8, BLK);
+          copy_block(ring_at + s * BLK, p_src, BLK, bar_at + s * 8);
+        } else {
+          mbar_arrive(bar_at + s * 8);           // (a unit's pages are odd)
+        }
       }
-      if (++p_page == p_pages) {
-        p_page = 0;
+      p_page += S;
+      if (p_page - half >= p_pages) {
+        p_page = half;
         if (++p_tile == p_tiles) {
           p_tile = 0;
           if (++p_hk == a.Hkv) {
@@ -254,12 +277,12 @@ attn_int4_kernel(const AttnArgs a) {
             do { ++p_b; } while (p_b < a.B && s_nr[p_b] == 0);
             if (p_b >= a.B) return;             // (the last page of all: nothing is requested after it)
             p_window = -1;
-            p_pages = (s_ctx[p_b] + s_nr[p_b] + 15) >> 4;
+            p_pages = pages_of(p_b);
             p_tiles = tiles_of(s_nr[p_b]);
           }
         }
         aim();
-      } else if ((p_page & 31) == 0) {
+      } else if ((p_page & 31) < S) {
         aim();
       }
     };
@@ -272,65 +295,70 @@ attn_int4_kernel(const AttnArgs a) {
     uint32_t parity = 0;
     bool ok = true;
     while (it < n && ok) {
-      // ---- a unit, or what of it is this warp's ----
+      // ---- a unit, or what of it is this team's ----
       const int row0 = tile * TM, nr = s_nr[b], ctx = s_ctx[b], nrows = nr * a.G;
-      const int first = page, last = min(pages, page + (n - it));
-      if (lane == 0) {
-        const Segment seg{b, hk, row0, per_warp * warp + it - page, pages};
-        if (it == 0) s_seg[warp][0] = seg;
-        if (n - it <= pages - page) s_seg[warp][1] = seg;
+      const int first = blk, last = min(blocks, blk + (n - it));
+      if (half == 0 && lane == 0) {
+        const Segment seg{b, hk, row0, per_team * team + it - blk, blocks};
+        if (it == 0) s_seg[team][0] = seg;
+        if (n - it <= blocks - blk) s_seg[team][1] = seg;
       }
       // Q: a lane's features are those of its K words
-      uint32_t qa[Z::kQInSmem ? 1 : NT][DH / 8];
-      uint4* const my_q = reinterpret_cast<uint4*>(my_ring + ST * BLK) + lane;
+      uint32_t qa[Z::kQInSmem ? 1 : DH / 8];
+      uint4* const my_q = reinterpret_cast<uint4*>(region + S * ST * BLK) + lane;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const int row = row0 + 8 * t + g, i = verify_row(row), j = row - i * a.G;
         const bf16* src = a.q + (size_t(b) * a.Rs + i) * a.ldq + size_t(hk * a.G + j) * DH + qd * (DH / 4);
 #pragma unroll
-        for (int x = 0; x < QC; ++x) {
+        for (int y = 0; y < QC / S; ++y) {
+          const int x = half * (QC / S) + y;
           const uint4 v = row < nrows ? reinterpret_cast<const uint4*>(src)[x] : make_uint4(0, 0, 0, 0);
           if (Z::kQInSmem) {
             my_q[(t * QC + x) * 32] = v;
           } else {
-            uint32_t* to = qa[Z::kQInSmem ? 0 : t] + 4 * x;
-            to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
+            uint32_t* to = qa + (Z::kQInSmem ? 0 : 4 * x);
+            to[0] = v.x; to[Z::kQInSmem ? 0 : 1] = v.y; to[Z::kQInSmem ? 0 : 2] = v.z; to[Z::kQInSmem ? 0 : 3] = v.w;
           }
         }
       }
       if (a.parents && path_b != b) {
-        unsigned long long mask[2];
-        tree_paths(a.parents + size_t(b) * a.Rs, nr, lane, mask);
-        __syncwarp();
-        s_path[warp][lane] = mask[0];
-        s_path[warp][lane + 32] = mask[1];
-        __syncwarp();
+        if (half == 0) {
+          unsigned long long mask[2];
+          tree_paths(a.parents + size_t(b) * a.Rs, nr, lane, mask);
+          __syncwarp();
+          s_path[team][lane] = mask[0];
+          s_path[team][lane + 32] = mask[1];
+          __syncwarp();
+        }
         path_b = b;
       }
+      if (S == 2) team_sync(team);
       // shift = -m, with m the softmax's reference: p = 2^(score x scale + shift)
-      float o[NT][MT][4], sums[NT][4], shift[NT][2];
+      float o[NT][OT][4], sums[NT][4], shift[NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         shift[t][0] = shift[t][1] = kNothing;
         sums[t][0] = sums[t][1] = sums[t][2] = sums[t][3] = 0.f;
 #pragma unroll
-        for (int f = 0; f < MT; ++f) o[t][f][0] = o[t][f][1] = o[t][f][2] = o[t][f][3] = 0.f;
+        for (int f = 0; f < OT; ++f) o[t][f][0] = o[t][f][1] = o[t][f][2] = o[t][f][3] = 0.f;
       }
 
 #pragma unroll 1
-      for (; page < last; ++page, ++it) {
-        if (!mbar_wait_warp(bar_at + stage * 8, parity, &s_abort)) { ok = false; break; }
-        const uint8_t* blk = my_ring + stage * BLK;
+      for (; blk < last; ++blk, ++it) {
+        ok = mbar_wait_warp(bar_at + stage * 8, parity, &s_abort);
+        if (S == 1 && !ok) break;              // (a team's warps go on to their next vote)
+        const uint8_t* mine = region + (half * ST + stage) * BLK;
         // ---- scores: of tokens g and g + 8 (the halves of x) and the lane's rows 2 qd, 2 qd + 1 of each tile ----
         float x[NT][4];
         {
 #pragma unroll
           for (int t = 0; t < NT; ++t) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.f;
           uint32_t k0[KW], k1[KW];
-          lds<KW>(k0, blk + q4_k_codes(DH, g, qd * KW));
-          lds<KW>(k1, blk + q4_k_codes(DH, g + 8, qd * KW));
-          const uint32_t sz0 = *reinterpret_cast<const uint32_t*>(blk + q4_k_scale(DH, g, qd * (DH / 4) / 32));
-          const uint32_t sz1 = *reinterpret_cast<const uint32_t*>(blk + q4_k_scale(DH, g + 8, qd * (DH / 4) / 32));
+          lds<KW>(k0, mine + q4_k_codes(DH, g, qd * KW));
+          lds<KW>(k1, mine + q4_k_codes(DH, g + 8, qd * KW));
+          const uint32_t sz0 = *reinterpret_cast<const uint32_t*>(mine + q4_k_scale(DH, g, qd * (DH / 4) / 32));
+          const uint32_t sz1 = *reinterpret_cast<const uint32_t*>(mine + q4_k_scale(DH, g + 8, qd * (DH / 4) / 32));
           const uint32_t s0 = __byte_perm(sz0, 0, 0x1010), z0 = __byte_perm(sz0, 0, 0x3232);
           const uint32_t s1 = __byte_perm(sz1, 0, 0x1010), z1 = __byte_perm(sz1, 0, 0x3232);
 #pragma unroll
@@ -342,8 +370,8 @@ attn_int4_kernel(const AttnArgs a) {
             uint4 q[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-              const uint32_t* own = qa[Z::kQInSmem ? 0 : t] + 4 * w;
-              q[t] = Z::kQInSmem ? my_q[(t * QC + w) * 32] : make_uint4(own[0], own[1], own[2], own[3]);
+              const uint32_t* own = qa + (Z::kQInSmem ? 0 : 4 * w);
+              q[t] = Z::kQInSmem ? my_q[(t * QC + w) * 32] : make_uint4(own[0], own[Z::kQInSmem ? 0 : 1], own[Z::kQInSmem ? 0 : 2], own[Z::kQInSmem ? 0 : 3]);
             }
 #pragma unroll
             for (int t = 0; t < NT; ++t) mma16816(x[t], ka, q[t].x, q[t].y);
@@ -351,7 +379,8 @@ attn_int4_kernel(const AttnArgs a) {
             for (int t = 0; t < NT; ++t) mma16816(x[t], kb, q[t].z, q[t].w);
           }
         }
-        if (page * 16 + 15 >= ctx) {      // some of the step's own rows, or slots behind them
+        const int page = blk * S + half;        // (the second of a team's may be one too many: all of it is masked)
+        if (page * 16 + 15 >= ctx) {            // some of the step's own rows, or slots behind them
           const int rel0 = page * 16 + g - ctx, rel1 = rel0 + 8;
 #pragma unroll
           for (int t = 0; t < NT; ++t)
@@ -359,7 +388,7 @@ attn_int4_kernel(const AttnArgs a) {
             for (int y = 0; y < 2; ++y) {
               const int i = verify_row(min(row0 + 8 * t + 2 * qd + y, nrows - 1));      // (rows that are not active: as the last)
               if (a.parents) {
-                const unsigned long long see = s_path[warp][i];
+                const unsigned long long see = s_path[team][i];
                 if (rel0 >= 0 && (rel0 >= 64 || !(see >> (rel0 & 63) & 1))) x[t][y] = -INFINITY;
                 if (rel1 >= 0 && (rel1 >= 64 || !(see >> (rel1 & 63) & 1))) x[t][2 + y] = -INFINITY;
               } else {
@@ -368,68 +397,116 @@ attn_int4_kernel(const AttnArgs a) {
               }
             }
         }
-        bool above = false;
+        bool above = !ok;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int y = 0; y < 2; ++y) above = above || fmaf(fmaxf(x[t][y], x[t][2 + y]), a.scale, shift[t][y]) > 6.f;
-        if (__any_sync(0xffffffffu, above)) {
+        // probabilities: from (token, row) to the second product's fragments, a row's tokens 2 qd, 2 qd + 1 (and 8 on) in lane g
+        uint32_t p[NT][2];
+        uint2* const team_p = reinterpret_cast<uint2*>(region + S * ST * BLK + Z::kQBytes + (it & 1) * Z::kPBytes) + lane;
+        auto probabilities = [&]() {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            p[t][0] = transpose8(pack_bf16(ex2(fmaf(x[t][0], a.scale, shift[t][0])), ex2(fmaf(x[t][1], a.scale, shift[t][1]))));
+            p[t][1] = transpose8(pack_bf16(ex2(fmaf(x[t][2], a.scale, shift[t][0])), ex2(fmaf(x[t][3], a.scale, shift[t][1]))));
+            if (S == 2) team_p[(half * NT + t) * 32] = make_uint2(p[t][0], p[t][1]);
+          }
+        };
+        // (a team's are there with the vote, and again if that says so)
+        if (S == 2) probabilities();
+        if (S == 1 ? __any_sync(0xffffffffu, above) : team_any(team, above)) {
+          if (S == 2 && team_any(team, !ok)) { ok = false; break; }
+          float top[NT][2];
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              top[t][y] = fmaxf(x[t][y], x[t][2 + y]);
+#pragma unroll
+              for (int d = 4; d <= 16; d <<= 1) top[t][y] = fmaxf(top[t][y], __shfl_xor_sync(0xffffffffu, top[t][y], d));
+              if (S == 2 && g == 0) s_half[S == 1 ? 0 : warp][8 * t + 2 * qd + y] = top[t][y];
+            }
+          if (S == 2) team_sync(team);
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             float down[2];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              float top = fmaxf(x[t][y], x[t][2 + y]);
-#pragma unroll
-              for (int d = 4; d <= 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-              const float next = fminf(shift[t][y], -ceilf(top * a.scale));
+              if (S == 2) top[t][y] = fmaxf(top[t][y], s_half[S == 1 ? 0 : warp ^ 1][8 * t + 2 * qd + y]);
+              const float next = fminf(shift[t][y], -ceilf(top[t][y] * a.scale));
               down[y] = ex2(next - shift[t][y]);
               shift[t][y] = next;
             }
 #pragma unroll
             for (int c = 0; c < 4; ++c) sums[t][c] *= down[c & 1];
 #pragma unroll
-            for (int f = 0; f < MT; ++f)
+            for (int f = 0; f < OT; ++f)
 #pragma unroll
               for (int c = 0; c < 4; ++c) o[t][f][c] *= down[c & 1];
           }
+          if (S == 2) {
+            probabilities();
+            team_sync(team);
+          }
         }
-        // ---- probabilities: from (token, row) to the second product's fragments, a row's tokens 2 qd, 2 qd + 1 (and 8 on) in lane g ----
-        uint32_t p0[NT], p1[NT];
+        if (S == 1) probabilities();
+        // (with that vote both are done with the block before)
+        if (S == 2 && it > 0 && it - 1 + ST < n) request(stage == 0 ? ST - 1 : stage - 1);
+        const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          p0[t] = transpose8(pack_bf16(ex2(fmaf(x[t][0], a.scale, shift[t][0])), ex2(fmaf(x[t][1], a.scale, shift[t][1]))));
-          p1[t] = transpose8(pack_bf16(ex2(fmaf(x[t][2], a.scale, shift[t][0])), ex2(fmaf(x[t][3], a.scale, shift[t][1]))));
-        }
+        for (int t = 0; t < NT; ++t) mma16816(sums[t], ones, p[t][0], p[t][1]);
         // ---- values ----
-        {
-          uint32_t v0[KW], v1[KW], sz[4];
-          lds<KW>(v0, blk + 10 * DH + lane * KW * 4);
-          lds<KW>(v1, blk + 10 * DH + (32 + lane) * KW * 4);
-          lds<4>(sz, blk + 18 * DH + (g * CPG / 32 * 4 + qd) * 16);
-          const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
-          for (int t = 0; t < NT; ++t) mma16816(sums[t], ones, p0[t], p1[t]);
+        for (int h = 0; h < S; ++h) {
+          if (h == 1 && 2 * blk + 1 >= pages) break;
+          const uint8_t* from = region + (h * ST + stage) * BLK;
+          uint32_t v0[VW], v1[VW], sz[4];
+          lds<VW>(v0, from + 10 * DH + lane * KW * 4 + half * VW * 4);
+          lds<VW>(v1, from + 10 * DH + (32 + lane) * KW * 4 + half * VW * 4);
+          lds<4>(sz, from + 18 * DH + (g * CPG / 32 * 4 + qd) * 16);
+          if (S == 2) {
 #pragma unroll
-          for (int w = 0; w < KW; ++w) {
+            for (int t = 0; t < NT; ++t) {
+              const uint2 u = team_p[(h * NT + t) * 32];
+              p[t][0] = u.x; p[t][1] = u.y;
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < VW; ++w) {
             const uint32_t va[4] = {values(v0[w] << 3, sz[0], sz[1]), values(v0[w] >> 1, sz[0], sz[1]), values(v1[w] << 3, sz[2], sz[3]),
                                     values(v1[w] >> 1, sz[2], sz[3])};
             const uint32_t vb[4] = {values(v0[w] >> 5, sz[0], sz[1]), values(v0[w] >> 9, sz[0], sz[1]), values(v1[w] >> 5, sz[2], sz[3]),
                                     values(v1[w] >> 9, sz[2], sz[3])};
 #pragma unroll
-            for (int t = 0; t < NT; ++t) mma16816(o[t][2 * w], va, p0[t], p1[t]);
+            for (int t = 0; t < NT; ++t) mma16816(o[t][2 * w], va, p[t][0], p[t][1]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) mma16816(o[t][2 * w + 1], vb, p0[t], p1[t]);
+            for (int t = 0; t < NT; ++t) mma16816(o[t][2 * w + 1], vb, p[t][0], p[t][1]);
           }
         }
-        __syncwarp();
-        if (it + ST < n) request(stage);
+        if (S == 1) {
+          __syncwarp();
+          if (it + ST < n) request(stage);
+        }
         if (++stage == ST) { stage = 0; parity ^= 1; }
       }
       if (!ok) break;
 
-      // ---- the unit's result, or the piece that this warp has of it ----
-      if (first == 0 && last == pages) {
+      // ---- the unit's result, or the piece that this team has of it ----
+      if (S == 2) {                            // the sums: each warp's pages'
+        if (g == 0) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) s_half[S == 1 ? 0 : warp][8 * t + 2 * qd + y] = sums[t][y];
+        }
+        team_sync(team);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) sums[t][y] += s_half[S == 1 ? 0 : warp ^ 1][8 * t + 2 * qd + y];
+      }
+      if (first == 0 && last == blocks) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -438,50 +515,51 @@ attn_int4_kernel(const AttnArgs a) {
             if (row >= nrows) continue;
             const float inv = 1.f / sums[t][y];      // (a row sees itself: its sum is not zero)
             const int i = verify_row(row), j = row - i * a.G;
-            bf16* dst = a.out + (size_t(b) * a.Rs + i) * a.ldo + size_t(hk * a.G + j) * DH + CPG * g;
-            uint32_t w[MT];
+            bf16* dst = a.out + (size_t(b) * a.Rs + i) * a.ldo + size_t(hk * a.G + j) * DH + CPG * g + 2 * OT * half;
+            uint32_t w[OT];
 #pragma unroll
-            for (int f = 0; f < MT; ++f) w[f] = pack_bf16(o[t][f][y] * inv, o[t][f][2 + y] * inv);
-            if (a.vec_out) {
+            for (int f = 0; f < OT; ++f) w[f] = pack_bf16(o[t][f][y] * inv, o[t][f][2 + y] * inv);
+            if (a.vec_out && OT >= 4) {
 #pragma unroll
-              for (int f = 0; f < MT; f += 4) *reinterpret_cast<uint4*>(dst + 2 * f) = make_uint4(w[f], w[f + 1], w[f + 2], w[f + 3]);
+              for (int f = 0; f < OT; f += 4) *reinterpret_cast<uint4*>(dst + 2 * f) = make_uint4(w[f], w[(f + 1) % OT], w[(f + 2) % OT], w[(f + 3) % OT]);
             } else {
 #pragma unroll
-              for (int f = 0; f < MT; ++f) *reinterpret_cast<uint32_t*>(dst + 2 * f) = w[f];
+              for (int f = 0; f < OT; ++f) *reinterpret_cast<uint32_t*>(dst + 2 * f) = w[f];
             }
           }
       } else {
-        const bool early = it < n;      // the warp goes on: its memory is not free yet
+        const bool early = it < n;      // the team goes on: its memory is not free yet
         __syncwarp();
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           if (row0 + 8 * t >= nrows) break;      // (no row of the tile)
 #pragma unroll
-          for (int f = 0; f < MT; ++f) {
+          for (int f = 0; f < OT; ++f) {
             const float4 v = make_float4(o[t][f][0], o[t][f][1], o[t][f][2], o[t][f][3]);
-            if (early) __stcg(my_part + (t * MT + f) * 32, v);
-            else reinterpret_cast<float4*>(my_ring)[(t * MT + f) * 32 + lane] = v;
+            const int sl = t * MT + half * OT + f;
+            if (early) __stcg(my_part + sl * 32, v);
+            else reinterpret_cast<float4*>(region)[sl * 32 + lane] = v;
           }
-          if (g == 0) {
+          if (half == 0 && g == 0) {
 #pragma unroll
-            for (int y = 0; y < 2; ++y) s_ml[warp][early ? 0 : 1][8 * t + 2 * qd + y] = make_float2(shift[t][y] == kNothing ? -INFINITY : -shift[t][y], sums[t][y]);
+            for (int y = 0; y < 2; ++y) s_ml[team][early ? 0 : 1][8 * t + 2 * qd + y] = make_float2(shift[t][y] == kNothing ? -INFINITY : -shift[t][y], sums[t][y]);
           }
         }
       }
-      if (page == pages) {
-        page = 0;
+      if (blk == blocks) {
+        blk = 0;
         if (++tile == tiles) {
           tile = 0;
           if (++hk == a.Hkv) {
             hk = 0;
             do { ++b; } while (b < a.B && s_nr[b] == 0);
-            if (b < a.B) { pages = (s_ctx[b] + s_nr[b] + 15) >> 4; tiles = tiles_of(s_nr[b]); }
+            if (b < a.B) { pages = pages_of(b); blocks = (pages + S - 1) / S; tiles = tiles_of(s_nr[b]); }
           }
         }
       }
     }
     if (!ok && lane == 0)     // copies in flight land before the CTA's memory goes
-      for (int x = it; x < min(n, it + ST); ++x) {
+      for (int x = it; x < min(n, S == 2 && it > 0 ? it - 1 + ST : it + ST); ++x) {
         mbar_drain(bar_at + stage * 8, parity);
         if (++stage == ST) { stage = 0; parity ^= 1; }
       }
@@ -492,21 +570,21 @@ attn_int4_kernel(const AttnArgs a) {
     return;
   }
 
-  // ---- this CTA's pieces: of units around its ends and around the places where one warp follows another ----
+  // ---- this CTA's pieces: of units around its ends and around the places where one team follows another ----
   if (warp == 0) {
-    const int w = lane >> 1, begin_w = w * per_warp;
+    const int w = lane >> 1, begin_w = w * per_team;
     Cut c{};
-    bool here = lane < 2 * W && begin_w < span;
+    bool here = lane < 2 * T && begin_w < span;
     if (here) {
       c.seg = s_seg[w][lane & 1];
-      const int end = c.seg.start + c.seg.pages;
+      const int end = c.seg.start + c.seg.blocks;
       here = lane == 0 || s_seg[(lane - 1) >> 1][(lane - 1) & 1].start != c.seg.start;        // (the first to list it)
       c.first = w;
-      c.last = (min(end, span) - 1) / per_warp;
+      c.last = (min(end, span) - 1) / per_team;
       c.begun = c.seg.start < 0;
       c.open = c.begun || end > span;
-      c.early = end < min((c.last + 1) * per_warp, span);
-      here = here && (c.open || c.first != c.last);       // (else one warp had it all)
+      c.early = end < min((c.last + 1) * per_team, span);
+      here = here && (c.open || c.first != c.last);       // (else one team had it all)
     }
     const unsigned all = __ballot_sync(0xffffffffu, here);
     if (here) s_cut[__popc(all & ((1u << lane) - 1))] = c;
@@ -517,13 +595,13 @@ attn_int4_kernel(const AttnArgs a) {
   // Four slices of eight rows at a time, the warps in turn.  First pieces' come from L2, as many together as there is room for.
   constexpr int kParts = Z::kSlices / 4, kTogether = Z::kFetched / 4;
   const int mine = (cuts * kParts - warp + W - 1) / W;
-  float4* const fetched = reinterpret_cast<float4*>(smem + warp * Z::kRegion + Z::kOBytes) + lane;
+  float4* const fetched = reinterpret_cast<float4*>(smem + team * Z::kRegion + Z::kOBytes + half * (Z::kFetched * 512)) + lane;
   auto fetch = [&](int x0) {
 #pragma unroll 1
     for (int x = x0; x < min(x0 + kTogether, mine); ++x) {
       const int c = (warp + x * W) / kParts, part = warp + x * W - c * kParts;
       if (!s_cut[c].early) continue;
-      const float4* from = reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * W + s_cut[c].last) * Z::kSlices + 4 * part) * 32 + lane;
+      const float4* from = reinterpret_cast<const float4*>(a.part) + (size_t(blockIdx.x * T + s_cut[c].last) * Z::kSlices + 4 * part) * 32 + lane;
 #pragma unroll
       for (int k = 0; k < 4; ++k) copy16(smem_u32(fetched + ((x - x0) * 4 + k) * 32), from + k * 32);
     }
@@ -595,7 +673,7 @@ attn_int4_kernel(const AttnArgs a) {
   // the unit that goes on behind this CTA
   if (tid == 0 && cuts > 0 && s_cut[cuts - 1].open && !s_cut[cuts - 1].begun) {
     const Segment& seg = s_cut[cuts - 1].seg;
-    a.joins[blockIdx.x] = Join{seg.b, seg.hk, seg.row0, s_nr[seg.b] * a.G, (seg.start + seg.pages - 1) / per_cta + 1};
+    a.joins[blockIdx.x] = Join{seg.b, seg.hk, seg.row0, s_nr[seg.b] * a.G, (seg.start + seg.blocks - 1) / per_cta + 1};
   }
 }
 
