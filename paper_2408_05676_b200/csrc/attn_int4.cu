@@ -39,7 +39,7 @@ struct Sizes {
   // A team is a warp, or two that take a page each of every two and half of the features each
   static constexpr int kTeam = NT == 1 ? 1 : 2;
   static constexpr int kRegsO = NT * DH / 4 / kTeam;     // O registers of a lane
-  static constexpr int kWarps = kRegsO <= 32 ? 16 : kRegsO <= 48 ? 12 : 8;      // as many as the registers allow without spills
+  static constexpr int kWarps = NT == 1 ? 16 : kRegsO <= 48 ? 12 : 8;      // as many as the registers allow without spills
   static constexpr int kTeams = kWarps / kTeam;
   static constexpr int kRows = 8 * NT;
   static constexpr int kBlock = q4_block_bytes(DH);      // bytes of a page and head
@@ -54,7 +54,7 @@ struct Sizes {
   static constexpr int kFetched = kTeam == 1 ? 16 : 8;   // slices of a warp
   static constexpr int kRegion = kLoop > kOBytes + kTeam * kFetched * 512 ? kLoop : kOBytes + kTeam * kFetched * 512;
   static constexpr int kRecord = kOBytes / 4 + 16 * NT;  // floats of a CTA's piece: O, then (m, sum) of the rows
-  static constexpr int smem(int B) { return kTeams * kRegion + kWarps * kStages * 8 + (B + 1) * 8 + B * 12; }
+  static constexpr int smem(int B) { return kTeams * kRegion + (B + 1) * 8 + B * 12; }
   static constexpr int kPart = kTeams * (kOBytes / 4);   // floats of a CTA's teams' first pieces
   static size_t part_floats(int ctas) { return size_t(ctas) * (kPart + 2 * kRecord) + size_t(ctas) * (sizeof(Join) / 4); }
 };
@@ -99,13 +99,12 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
-__device__ __forceinline__ void copy_block(uint32_t dst, const void* src, int bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void lds(uint32_t (&w)[N], const uint8_t* p) {
@@ -148,8 +147,7 @@ attn_int4_kernel(const AttnArgs a) {
   constexpr int OT = MT / S;             // a warp's
   constexpr int QC = DH / 32;            // 16-byte pieces of a lane's share of a Q row
   extern __shared__ __align__(128) uint8_t smem[];
-  uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + T * Z::kRegion);        // [W][ST], behind the teams' regions
-  long long* const s_pre = reinterpret_cast<long long*>(bars + W * ST);             // [B + 1] blocks before a sequence
+  long long* const s_pre = reinterpret_cast<long long*>(smem + T * Z::kRegion);     // [B + 1] blocks before a sequence, behind the teams' regions
   int* const s_ctx = reinterpret_cast<int*>(s_pre + a.B + 1);                       // [B]
   int* const s_nr = s_ctx + a.B;                                                    // [B]
   int* const s_seq = s_nr + a.B;                                                    // [B]
@@ -159,17 +157,12 @@ attn_int4_kernel(const AttnArgs a) {
   __shared__ Cut s_cut[2 * T];
   __shared__ __align__(16) float2 s_ml[T][2][TM];   // m and sum of the rows of the piece that a team began with, if it went on; that it ended with
   __shared__ float s_half[S == 1 ? 1 : W][TM];      // what a warp tells the other of its rows: highest scores, or sums
-  __shared__ int s_abort, s_cuts;
+  __shared__ int s_cuts;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3, team = warp / S, half = warp % S;
   // a row is verify row row / G, head row % G of its kv head
   auto verify_row = [&](int row) { return a.G == 1 ? row : int(__umulhi(unsigned(row), a.group_inv)); };
 
   next_may_launch();
-  if (tid == 0) s_abort = 0;
-  if (lane < ST) {
-    mbar_init(smem_u32(&bars[warp * ST + lane]), 1);
-    mbar_fence_init();
-  }
   // a step's tables were complete before any kernel of the forward began
   if (!a.row_ctx) wait_for_earlier();
 
@@ -232,7 +225,7 @@ attn_int4_kernel(const AttnArgs a) {
 
   if (n > 0) {
     uint8_t* const region = smem + team * Z::kRegion;
-    const uint32_t ring_at = smem_u32(region) + half * (ST * BLK), bar_at = smem_u32(bars + warp * ST);
+    const uint32_t ring_at = smem_u32(region) + half * (ST * BLK) + lane * 16;
     // ---- where the team begins ----
     int b, tile, hk, blk;
     {
@@ -248,24 +241,21 @@ attn_int4_kernel(const AttnArgs a) {
     }
     int pages = pages_of(b), blocks = (pages + S - 1) / S, tiles = tiles_of(s_nr[b]);
 
-    // ---- copies: a cursor that runs ST blocks ahead; of 32 pages each lane holds one's address and requests that page ----
+    // ---- copies: a cursor that runs ST blocks ahead; of 32 pages each lane holds one's number ----
     int p_b = b, p_tile = tile, p_hk = hk, p_page = blk * S + half, p_pages = pages, p_tiles = tiles, p_window = -1, p_id = 0;
-    const uint8_t* p_src = nullptr;
     auto aim = [&]() {
       if (p_window != (p_page & ~31)) {
         p_window = p_page & ~31;
         p_id = a.page_table[size_t(s_seq[p_b]) * a.pages_per_seq + min(p_window + lane, p_pages - 1)];
       }
-      p_src = a.pages + (size_t(p_id) * a.Hkv + p_hk) * BLK;
     };
     auto request = [&](int s) {
-      if (lane == (p_page & 31)) {
-        if (S == 1 || p_page < p_pages) {
-          mbar_expect_tx(bar_at + s * 8, BLK);
-          copy_block(ring_at + s * BLK, p_src, BLK, bar_at + s * 8);
-        } else {
-          mbar_arrive(bar_at + s * 8);           // (a unit's pages are odd)
-        }
+      const int id = __shfl_sync(0xffffffffu, p_id, p_page & 31);
+      if (S == 1 || p_page < p_pages) {          // (not so where a unit's pages are odd)
+        const uint8_t* src = a.pages + (size_t(id) * a.Hkv + p_hk) * BLK + lane * 16;
+#pragma unroll
+        for (int x = 0; x + 512 <= BLK; x += 512) copy16(ring_at + s * BLK + x, src + x);
+        if (BLK % 512 && lane < BLK % 512 / 16) copy16(ring_at + s * BLK + BLK / 512 * 512, src + BLK / 512 * 512);
       }
       p_page += S;
       if (p_page - half >= p_pages) {
@@ -289,12 +279,13 @@ attn_int4_kernel(const AttnArgs a) {
     __syncwarp();
     aim();
 #pragma unroll 1
-    for (int s = 0; s < min(n, ST); ++s) request(s);
+    for (int s = 0; s < ST; ++s) {
+      if (s < n) request(s);
+      copies_end();
+    }
 
     int it = 0, path_b = -1, stage = 0;
-    uint32_t parity = 0;
-    bool ok = true;
-    while (it < n && ok) {
+    while (it < n) {
       // ---- a unit, or what of it is this team's ----
       const int row0 = tile * TM, nr = s_nr[b], ctx = s_ctx[b], nrows = nr * a.G;
       const int first = blk, last = min(blocks, blk + (n - it));
@@ -346,8 +337,8 @@ attn_int4_kernel(const AttnArgs a) {
 
 #pragma unroll 1
       for (; blk < last; ++blk, ++it) {
-        ok = mbar_wait_warp(bar_at + stage * 8, parity, &s_abort);
-        if (S == 1 && !ok) break;              // (a team's warps go on to their next vote)
+        copies_but<ST - S>();
+        __syncwarp();
         const uint8_t* mine = region + (half * ST + stage) * BLK;
         // ---- scores: of tokens g and g + 8 (the halves of x) and the lane's rows 2 qd, 2 qd + 1 of each tile ----
         float x[NT][4];
@@ -397,11 +388,11 @@ attn_int4_kernel(const AttnArgs a) {
               }
             }
         }
-        bool above = !ok;
+        float highest = 0.f;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int y = 0; y < 2; ++y) above = above || fmaf(fmaxf(x[t][y], x[t][2 + y]), a.scale, shift[t][y]) > 6.f;
+          for (int y = 0; y < 2; ++y) highest = fmaxf(highest, fmaf(fmaxf(x[t][y], x[t][2 + y]), a.scale, shift[t][y]));
         // probabilities: from (token, row) to the second product's fragments, a row's tokens 2 qd, 2 qd + 1 (and 8 on) in lane g
         uint32_t p[NT][2];
         uint2* const team_p = reinterpret_cast<uint2*>(region + S * ST * BLK + Z::kQBytes + (it & 1) * Z::kPBytes) + lane;
@@ -415,8 +406,7 @@ attn_int4_kernel(const AttnArgs a) {
         };
         // (a team's are there with the vote, and again if that says so)
         if (S == 2) probabilities();
-        if (S == 1 ? __any_sync(0xffffffffu, above) : team_any(team, above)) {
-          if (S == 2 && team_any(team, !ok)) { ok = false; break; }
+        if (S == 1 ? __any_sync(0xffffffffu, highest > 6.f) : team_any(team, highest > 6.f)) {
           float top[NT][2];
 #pragma unroll
           for (int t = 0; t < NT; ++t)
@@ -452,7 +442,10 @@ attn_int4_kernel(const AttnArgs a) {
         }
         if (S == 1) probabilities();
         // (with that vote both are done with the block before)
-        if (S == 2 && it > 0 && it - 1 + ST < n) request(stage == 0 ? ST - 1 : stage - 1);
+        if (S == 2 && it > 0) {
+          if (it - 1 + ST < n) request(stage == 0 ? ST - 1 : stage - 1);
+          copies_end();
+        }
         const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
         for (int t = 0; t < NT; ++t) mma16816(sums[t], ones, p[t][0], p[t][1]);
@@ -487,10 +480,10 @@ attn_int4_kernel(const AttnArgs a) {
         if (S == 1) {
           __syncwarp();
           if (it + ST < n) request(stage);
+          copies_end();
         }
-        if (++stage == ST) { stage = 0; parity ^= 1; }
+        if (++stage == ST) stage = 0;
       }
-      if (!ok) break;
 
       // ---- the unit's result, or the piece that this team has of it ----
       if (S == 2) {                            // the sums: each warp's pages'
@@ -558,17 +551,8 @@ attn_int4_kernel(const AttnArgs a) {
         }
       }
     }
-    if (!ok && lane == 0)     // copies in flight land before the CTA's memory goes
-      for (int x = it; x < min(n, S == 2 && it > 0 ? it - 1 + ST : it + ST); ++x) {
-        mbar_drain(bar_at + stage * 8, parity);
-        if (++stage == ST) { stage = 0; parity ^= 1; }
-      }
   }
   __syncthreads();
-  if (s_abort) {
-    if (tid == 0) atomicCAS(a.status, 0, LASER_ERR_TIMEOUT);
-    return;
-  }
 
   // ---- this CTA's pieces: of units around its ends and around the places where one team follows another ----
   if (warp == 0) {
