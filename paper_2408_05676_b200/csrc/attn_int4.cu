@@ -87,6 +87,11 @@ __device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
 }
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
 // two codes at bits 3 .. 6 of the halves -> the two values.  (w & 0x00780078) | 0x41804180 as one instruction: of two constants the
 // compiler makes two, and the kernel's busiest pipe is the one for logic and shifts.
 __device__ __forceinline__ uint32_t values(uint32_t w, uint32_t s2, uint32_t z2) {
@@ -242,12 +247,13 @@ attn_int4_kernel(const AttnArgs a) {
     int pages = pages_of(b), blocks = (pages + S - 1) / S, tiles = tiles_of(s_nr[b]);
 
     // ---- copies: a cursor that runs ST blocks ahead; of 32 pages each lane holds one's number ----
-    int p_b = b, p_tile = tile, p_hk = hk, p_page = blk * S + half, p_pages = pages, p_tiles = tiles, p_window = -1, p_id = 0;
+    int p_b = b, p_tile = tile, p_hk = hk, p_page = blk * S + half, p_pages = pages, p_tiles = tiles, p_stop = 0, p_window = -1, p_id = 0;
     auto aim = [&]() {
       if (p_window != (p_page & ~31)) {
         p_window = p_page & ~31;
         p_id = a.page_table[size_t(s_seq[p_b]) * a.pages_per_seq + min(p_window + lane, p_pages - 1)];
       }
+      p_stop = min(p_pages, p_window + 32);
     };
     auto request = [&](int s) {
       const int id = __shfl_sync(0xffffffffu, p_id, p_page & 31);
@@ -258,6 +264,7 @@ attn_int4_kernel(const AttnArgs a) {
         if (BLK % 512 && lane < BLK % 512 / 16) copy16(ring_at + s * BLK + BLK / 512 * 512, src + BLK / 512 * 512);
       }
       p_page += S;
+      if (p_page - half < p_stop) return;
       if (p_page - half >= p_pages) {
         p_page = half;
         if (++p_tile == p_tiles) {
@@ -271,10 +278,8 @@ attn_int4_kernel(const AttnArgs a) {
             p_tiles = tiles_of(s_nr[p_b]);
           }
         }
-        aim();
-      } else if ((p_page & 31) < S) {
-        aim();
       }
+      aim();
     };
     __syncwarp();
     aim();
@@ -388,25 +393,25 @@ attn_int4_kernel(const AttnArgs a) {
               }
             }
         }
-        float highest = 0.f;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) highest = fmaxf(highest, fmaf(fmaxf(x[t][y], x[t][2 + y]), a.scale, shift[t][y]));
         // probabilities: from (token, row) to the second product's fragments, a row's tokens 2 qd, 2 qd + 1 (and 8 on) in lane g
         uint32_t p[NT][2];
         uint2* const team_p = reinterpret_cast<uint2*>(region + S * ST * BLK + Z::kQBytes + (it & 1) * Z::kPBytes) + lane;
-        auto probabilities = [&]() {
+        auto probabilities = [&]() {        // whether one is above 2^6
+          uint32_t highest = 0;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            p[t][0] = transpose8(pack_bf16(ex2(fmaf(x[t][0], a.scale, shift[t][0])), ex2(fmaf(x[t][1], a.scale, shift[t][1]))));
-            p[t][1] = transpose8(pack_bf16(ex2(fmaf(x[t][2], a.scale, shift[t][0])), ex2(fmaf(x[t][3], a.scale, shift[t][1]))));
+            p[t][0] = pack_bf16(ex2(fmaf(x[t][0], a.scale, shift[t][0])), ex2(fmaf(x[t][1], a.scale, shift[t][1])));
+            p[t][1] = pack_bf16(ex2(fmaf(x[t][2], a.scale, shift[t][0])), ex2(fmaf(x[t][3], a.scale, shift[t][1])));
+            highest = max2(highest, max2(p[t][0], p[t][1]));
+            p[t][0] = transpose8(p[t][0]);
+            p[t][1] = transpose8(p[t][1]);
             if (S == 2) team_p[(half * NT + t) * 32] = make_uint2(p[t][0], p[t][1]);
           }
+          return max2(highest, 0x42804280u) != 0x42804280u;
         };
-        // (a team's are there with the vote, and again if that says so)
-        if (S == 2) probabilities();
-        if (S == 1 ? __any_sync(0xffffffffu, highest > 6.f) : team_any(team, highest > 6.f)) {
+        // (with the reference as it is; again if that turns out too low)
+        const bool above = probabilities();
+        if (S == 1 ? __any_sync(0xffffffffu, above) : team_any(team, above)) {
           float top[NT][2];
 #pragma unroll
           for (int t = 0; t < NT; ++t)
@@ -435,12 +440,9 @@ attn_int4_kernel(const AttnArgs a) {
 #pragma unroll
               for (int c = 0; c < 4; ++c) o[t][f][c] *= down[c & 1];
           }
-          if (S == 2) {
-            probabilities();
-            team_sync(team);
-          }
+          probabilities();
+          if (S == 2) team_sync(team);
         }
-        if (S == 1) probabilities();
         // (with that vote both are done with the block before)
         if (S == 2 && it > 0) {
           if (it - 1 + ST < n) request(stage == 0 ? ST - 1 : stage - 1);
