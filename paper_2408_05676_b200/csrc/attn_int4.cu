@@ -2,18 +2,29 @@
 // sees the sequence's cached tokens and, of the step's own rows, 0 .. i (chain) or its ancestors and itself (token tree).
 //
 // The rows of a sequence that share a kv head (rows x n_heads / n_kv_heads) form tiles of 8 NT rows, NT = 1 .. 5.  (sequence, kv head,
-// tile) is a unit; all units' pages, one after another, are divided evenly over the SMs (one CTA each) and within a CTA over its warps, so
-// ragged lengths leave nobody idle.  A warp walks its pages alone: a page's K and V of a head, codes and scales, are one bulk copy into
-// the warp's own ring of shared-memory stages, and the codes become bf16 pairs in registers in the order of the MMA's fragments.  16
-// tokens a step, S^T = K Q^T and O^T += V^T P^T: tokens and features are the 16-row operand, so that what was unpacked serves all of the
-// tile's rows, eight at a time, and few rows waste little.  The sum of P is the product with ones.
+// tile) is a unit; all units' pages, one after another, are divided evenly over the SMs (one CTA each) and within a CTA over its teams, so
+// ragged lengths leave nobody idle.  A team is a warp, or two where NT > 1.  It walks its pages alone: a page's K and V of a head, codes
+// and scales, come by 16-byte copies into the warp's own ring of shared-memory stages (a bulk copy and its barrier cost a warp 300 clocks
+// a page, these 100), and the codes become bf16 pairs in registers in the order of the MMA's fragments.  S^T = K Q^T and O^T += V^T P^T:
+// tokens and features are the 16-row operand, so that what was unpacked serves all of the tile's rows, eight at a time, and few rows waste
+// little.  The sum of P is the product with ones.  Of a team's two warps each takes one page of two, then both pages' P and half of the
+// features: half the registers of O a lane, and no page is unpacked twice (one text of 64 thousand tokens, 36 rows: 56 us instead of 66).
+//
+// What bounds it: the instructions.  A warp-level MMA of 16 x 8 x 16 keeps a scheduler from issuing for eight clocks; a page is 16 NT of
+// them, and some 350 other instructions, 200 of them to unpack 4096 codes.  One row at a time over long texts reads 5.0 TB/s of the 6.6 that
+// a copy reaches; 17 rows take 940 clocks a page and scheduler.  On tensor memory, whose MMAs issue once for 128 tokens, the hand-overs
+// between unpacking, products and softmax took longer than what they saved (17 rows: 205 us instead of 122; 36 rows: 69 instead of 52).
 //
 // The softmax's reference m is a whole number in the exponent of two: raising it multiplies p and O by powers of two, exactly, so a
 // row's result does not depend on where its walk was cut but for the order of fp32 sums.  It is raised only when a score exceeds it by
 // more than 2^6, which a vote finds; p stays below 2^7, and bf16's and fp32's range is left to what is far below.
 //
-// Where a unit is cut, the pieces (m, sum, O in fp32) meet twice, in the order of the pages both times: the warps' in their CTA after its
+// Where a unit is cut, the pieces (m, sum, O in fp32) meet twice, in the order of the pages both times: the teams' in their CTA after its
 // last page, the CTAs' in a kernel that follows.
+//
+// Times (us; floors by bytes at 6.56 TB/s in brackets): 32 heads of 128, 9 rows over one text of 512 tokens 9.3 (0.4), over 16 of 256 to 768
+// 21.7 (6.7); 40 heads, trees of 17 rows over 64 texts of 256 to 1024 122 (42); 32 heads of 8 kv heads, one row over 64 texts of 4096 to 8192
+// 101 (77), 9 rows over one of 65536 52 (13).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -29,7 +40,7 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kMaxSeqs = 1024;     // sequences (or prompt chunks) of a call: their offsets are in shared memory
-constexpr int kMostTiles = 5;      // of eight rows in a tile: O takes 160 registers then
+constexpr int kMostTiles = 5;      // of eight rows in a tile: O takes 80 registers then (of three at most, 36 rows' pages are unpacked twice: 71 us instead of 69)
 
 // a unit that several CTAs have pieces of (count = 0: none)
 struct Join { int b, hk, row0, rows, count; };
@@ -665,7 +676,7 @@ attn_int4_kernel(const AttnArgs a) {
 
 // The units that several CTAs have pieces of: a block a CTA that has a unit's first piece, and eight rows; a warp 16 features.  In a kernel of
 // its own, with a unit's slices over many SMs: the last of its CTAs to arrive, joining alone, took 25 us of 90 where eight units of 40 rows
-// were in 19 pieces each, and still 2 to 5 where they were in 2 or 3; this one takes XX.
+// were in 19 pieces each, and still 2 to 5 where they were in 2 or 3; this one takes 2.
 template <int DH, int NT>
 __global__ void __launch_bounds__(DH * 2)
 attn_int4_join_kernel(const AttnArgs a) {

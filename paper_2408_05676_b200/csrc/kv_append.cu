@@ -54,13 +54,18 @@ __device__ __forceinline__ Raw<T> fetch4(const T* p, int vec) {
   return r;
 }
 
+__device__ __forceinline__ uint32_t two_bf16(float x, float y) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
 template <typename T, int DH>
 __global__ void __launch_bounds__(kAppendThreads)
 kv_append_kernel(const AppendArgs a) {
   constexpr int LPH = DH / 4, HPW = 32 / LPH;       // lanes of a head, heads of a warp
   constexpr int W = kAppendThreads / 32;
   __shared__ float2 s_cs[kRowsMost][DH / 2];
-  __shared__ int s_par[64], s_pos[kRowsMost];       // a row's position
+  __shared__ int s_pos[kRowsMost];                  // a row's position
   __shared__ void* s_dst[kRowsMost];          // its page (null: the row is not one)
   __shared__ int s_slot[kRowsMost];                 // its place in the page
   next_may_launch();
@@ -169,13 +174,11 @@ kv_append_kernel(const AppendArgs a) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) y[c] = __fadd_rn(__fmul_rn(y[c], cs[c]), __fmul_rn(p[c], sn[c]));
         }
-        uint32_t held[4];
+        uint2 held;
         if (kKind == 0 || !a.pages4) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) held[c] = bf16_bits(y[c]);
+          held = make_uint2(two_bf16(y[0], y[1]), two_bf16(y[2], y[3]));
           if (kKind > 0 && live)
-            *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(page) + (size_t(kKind - 1) * a.Hkv + h) * 16 * DH + t * DH + 4 * l) =
-                make_uint2(held[0] | held[1] << 16, held[2] | held[3] << 16);
+            *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(page) + (size_t(kKind - 1) * a.Hkv + h) * 16 * DH + t * DH + 4 * l) = held;
         } else {
           q4_finite(y);
           const Q4Scale sc = q4_scale(y);
@@ -196,12 +199,9 @@ kv_append_kernel(const AppendArgs a) {
               *reinterpret_cast<uint16_t*>(p + 4) = uint16_t(sc.z);
             }
           }
-          if (to) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) held[c] = q4_held(code[c], sc);
-          }
+          if (to) held = make_uint2(q4_held(code[0], sc) | q4_held(code[1], sc) << 16, q4_held(code[2], sc) | q4_held(code[3], sc) << 16);
         }
-        if (to && live) *reinterpret_cast<uint2*>(to + (size_t(r) * count + h) * DH + 4 * l) = make_uint2(held[0] | held[1] << 16, held[2] | held[3] << 16);
+        if (to && live) *reinterpret_cast<uint2*>(to + (size_t(r) * count + h) * DH + 4 * l) = held;
       }
     }
   };
