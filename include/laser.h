@@ -302,8 +302,7 @@ laser_status laser_kv_append(laser_kv* kv, int32_t layer, const int32_t* seq_ids
  *        as they are
  * The work is divided evenly over the SMs whatever the lengths.  It keeps partial results in memory of
  * the cache's.  Asynchronous on `stream`.
- * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 1024, or tiles of rows x pages beyond 2^31 a sequence); on the device as above,
- * and TIMEOUT. */
+ * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 1024, or tiles of rows x pages beyond 2^31 a sequence); on the device as above. */
 laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int32_t* seq_ids, const int32_t* parents,
                                const int32_t* n_rows, int32_t B, int32_t rows, const void* q, int64_t q_stride,
                                void* out, int64_t out_stride, void* stream);
@@ -356,20 +355,21 @@ laser_status laser_profile_read(laser_model* m, int32_t cls, double* ms, int64_t
  * often v occurs in the generated part of the text and on the path (rows 1 .. i; with parents row
  * i's ancestors and itself; row 0, the pending token, is the text's last):
  *   x = logit;  v in the text or on the path:  x = x > 0 ? x / repetition[b] : x * repetition[b]
- *   x = (x - frequency[b] * n) - presence[b] (if n > 0);  x = x + bias_b(v);  v not allowed: x = -inf
+ *   x = x - frequency[b] * n - presence[b] (if n > 0) + bias_b(v);  v not allowed: x = -inf
+ * in fp32, the quotient as a product with 1 / repetition[b] and the last three terms as one number.
  *   logits, out  dev fp32[B, rows, V]; out may be logits itself (other overlaps are refused).  Rows that
  *            are not active are left as they are
  *   tokens, parents (or NULL), n_rows  as for laser_verify_step(_tree), rows = K + 1 <= 64
  *   hist, hist_len, hist_stride  the texts as laser_draft_temp takes them, pending token included
  *            (NULL: no text); prompt_len dev int32[B]: how much of each is prompt, which counts for the
  *            repetition penalty alone (NULL: all of it is generated)
- *   repetition, frequency, presence  dev fp32[B], each may be NULL (1, 0, 0)
+ *   repetition (above 0), frequency, presence  dev fp32[B], each may be NULL (1, 0, 0)
  *   bias_offsets dev int32[B+1], bias_ids int32, bias_values fp32: the biases of sequence b are
  *            entries bias_offsets[b] .. bias_offsets[b+1]-1; those of one token add up in the
  *            list's order.  NULL, all three: none
  *   allowed  dev words of 32 tokens, bit v % 32 of word v / 32 set = allowed; the mask of a row starts
  *            at b * mask_seq_stride + i * mask_row_stride words (row stride 0: one mask a sequence).
- *            NULL: all are allowed
+ *            Masks of rows that are not active are there too, and may be read.  NULL: all are allowed
  * Token ids outside [0, V), in the text, the drafts and the biases, are ignored.  A row of which the mask
  * leaves nothing is -inf throughout.  Asynchronous on `stream`; no scratch memory.
  * Errors: INVALID_ARG (rows outside 1 .. 64, an overlap, strides shorter than a mask). */

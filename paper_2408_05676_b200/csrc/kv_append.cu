@@ -390,7 +390,6 @@ LASER_API laser_status laser_kv_check(laser_kv* kv, void* stream) {
   LASER_CUDA(cudaStreamSynchronize(as_stream(stream)));
   if (st == 0) return LASER_OK;
   LASER_CUDA(cudaMemsetAsync(kv->status, 0, 4, as_stream(stream)));
-  set_error(st == LASER_ERR_CAPACITY ? "a sequence outgrew its KV pages"
-            : st == LASER_ERR_TIMEOUT ? "a device-side wait ran out" : "a call was given a bad sequence id or parent");
+  set_error(st == LASER_ERR_CAPACITY ? "a sequence outgrew its KV pages" : "a call was given a bad sequence id or parent");
   return st;
 }

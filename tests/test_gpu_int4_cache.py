@@ -299,6 +299,46 @@ def test_long_texts_are_shared_out_and_joined(L, heads, kv_heads, dim, rows, len
         assert torch.equal(out, L.attend_int4(kv, 0, ids, n, q))
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("rows", [8, 10, 16, 17, 24, 25, 32, 33, 40, 41])
+def test_every_size_of_a_tile(L, dim, rows):
+    """Tiles of 8 to 40 rows over texts of odd and even numbers of pages: some in many pieces, some of a page or two that share a warp's run."""
+    rng = np.random.default_rng(100 + rows)
+    lens = [3001, 3, 640, 17, 0, 1200, 31]
+    B = len(lens)
+    kv = make(L, 2, 2, dim, B, -(-(max(lens) + rows) // 16))
+    held = fill(L, kv, range(B), [l + rows for l in lens], rng, 2.0)
+    L.kv_set_len(kv, range(B), lens)
+    n_rows = [rows, 1, rows, rows - 1, rows, 0, 2]
+    q = bf(rng.standard_normal((B, rows, 2, dim)))
+    out = torch.full_like(q, 7.0)
+    L.attend_int4(kv, 0, dev_i32(range(B)), dev_i32(n_rows), q, out=out)
+    L.kv_check(kv)
+    check_rows(f64(out), f64(q), held, lens, n_rows, None)
+    for b in range(B):
+        assert (out[b, n_rows[b]:] == 7).all()
+
+
+@pytest.mark.parametrize("rows,heads", [(9, 2), (1, 8), (9, 4)])
+def test_the_most_sequences_with_heads_of_128(L, rows, heads):
+    rng = np.random.default_rng(21)
+    B = 1024
+    kv = make(L, heads, 1, 128, B, 2)
+    lens = np.where(np.arange(B) < 40, rng.integers(0, 33 - rows, B), 0)
+    x = bf(rng.standard_normal((40 * 32, 128)))
+    for i in range(40):
+        L.kv_import(kv, i, 0, 0, x[32 * i:32 * i + 32], x[32 * i:32 * i + 32])
+    L.kv_set_len_dev(kv, dev_i32(lens))
+    q = bf(rng.standard_normal((B, rows, heads, 128)))
+    out = torch.full_like(q, 2.0)
+    L.attend_int4(kv, 0, dev_i32(range(B)), dev_i32([rows] * B), q, out=out)
+    L.kv_check(kv)
+    got = f64(out)
+    held = [held_rows(L, kv, i, 0, int(lens[i]) + rows) for i in range(40)]
+    check_rows(got[:40], f64(q)[:40], held, lens[:40].tolist(), [rows] * 40, None)
+    assert (got[40:] == 0).all()      # (fresh pages hold zeros)
+
+
 def test_a_text_does_not_depend_on_its_neighbours(L):
     """Alone, among others, in another order, with drafts behind it: results differ by no more than a bf16 step, and hardly ever."""
     rng = np.random.default_rng(9)
