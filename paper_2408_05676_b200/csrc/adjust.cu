@@ -10,6 +10,8 @@
 // load and a store a logit, coalesced whatever the rows' alignment.  A trip to memory takes 1.6 us under load, so each thread has its
 // logits of the next kAhead rows on their way into shared memory (72 KB an SM; with one row ahead, in registers, 64 trees of 17 rows took
 // 71 us instead of 66).  A warp's 32 tokens are one word of the grammar mask, and logits that it forbids are not read.
+#include <type_traits>
+
 #include "model.cuh"
 #include "tma.cuh"
 #include "tree.cuh"
@@ -248,14 +250,15 @@ LASER_API laser_status laser_adjust_logits(const float* logits, const int32_t* t
   if (B == 0) return LASER_OK;
   AdjustArgs a{logits, out, tokens, parents, n_rows, hist, hist_len, prompt_len, hist_stride, repetition, frequency, presence,
                bias_offsets, bias_ids, bias_values, allowed, mask_seq_stride, mask_row_stride, rows, V};
-  auto launch = [&](auto kernel, int run, int smem) -> laser_status {
-    LASER_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    LASER_CUDA(launch_overlapped(kernel, dim3(unsigned(ceil_div(V, run)), unsigned(B)), kThreads, size_t(smem), as_stream(stream), a));
+  auto launch = [&](auto tokens_of_thread) -> laser_status {
+    constexpr int U = decltype(tokens_of_thread)::value;
+    LASER_CUDA(allow_shared_memory<adjust_kernel<U>>(int(sizeof(Tables<U>))));
+    LASER_CUDA(launch_overlapped(adjust_kernel<U>, dim3(unsigned(ceil_div(V, U * kThreads)), unsigned(B)), kThreads, sizeof(Tables<U>), as_stream(stream), a));
     return LASER_OK;
   };
   // runs of 2048 tokens; of 512 where the SMs would be left without work
-  if (int64_t(B) * ceil_div(V, 8 * kThreads) >= 148) LASER_TRY(launch(adjust_kernel<8>, 8 * kThreads, int(sizeof(Tables<8>))));
-  else LASER_TRY(launch(adjust_kernel<2>, 2 * kThreads, int(sizeof(Tables<2>))));
+  if (int64_t(B) * ceil_div(V, 8 * kThreads) >= 148) LASER_TRY(launch(std::integral_constant<int, 8>{}));
+  else LASER_TRY(launch(std::integral_constant<int, 2>{}));
   count_launch();
   return LASER_OK;
 }

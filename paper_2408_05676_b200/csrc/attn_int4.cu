@@ -755,29 +755,28 @@ laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t strea
     return LASER_ERR_CAPACITY;
   }
   a.vec_out = (reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo * 2)) % 16 == 0;
-  auto launch = [&](auto kernel, auto join, auto sizes) -> laser_status {
-    using Z = decltype(sizes);
-    const int smem = Z::smem(a.B);
+  auto launch = [&](auto dh, auto tiles) -> laser_status {
+    constexpr int DH = decltype(dh)::value, NT = decltype(tiles)::value;
+    using Z = Sizes<DH, NT>;
     const unsigned grid = unsigned(std::min<int64_t>(kv->attn_ctas, units * a.B * kv->pages_per_seq));
-    LASER_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     a.records = a.part + size_t(grid) * Z::kPart;
     a.joins = reinterpret_cast<Join*>(a.records + size_t(grid) * 2 * Z::kRecord);
-    LASER_CUDA(launch_overlapped(kernel, dim3(grid), Z::kWarps * 32, size_t(smem), stream, a));
+    LASER_CUDA((allow_shared_memory<attn_int4_kernel<DH, NT>>(Z::smem(kMaxSeqs))));
+    LASER_CUDA(launch_overlapped(attn_int4_kernel<DH, NT>, dim3(grid), Z::kWarps * 32, size_t(Z::smem(a.B)), stream, a));
     count_launch();
     if (grid > 1) {
-      LASER_CUDA(launch_overlapped(join, dim3(grid, nt), kv->head_dim * 2, size_t(grid) * 64, stream, a));
+      LASER_CUDA(launch_overlapped(attn_int4_join_kernel<DH, NT>, dim3(grid, NT), DH * 2, size_t(grid) * 64, stream, a));
       count_launch();
     }
     return LASER_OK;
   };
   auto by_tiles = [&](auto dh) -> laser_status {
-    constexpr int D = decltype(dh)::value;
     switch (nt) {
-      case 1: return launch(attn_int4_kernel<D, 1>, attn_int4_join_kernel<D, 1>, Sizes<D, 1>{});
-      case 2: return launch(attn_int4_kernel<D, 2>, attn_int4_join_kernel<D, 2>, Sizes<D, 2>{});
-      case 3: return launch(attn_int4_kernel<D, 3>, attn_int4_join_kernel<D, 3>, Sizes<D, 3>{});
-      case 4: return launch(attn_int4_kernel<D, 4>, attn_int4_join_kernel<D, 4>, Sizes<D, 4>{});
-      default: return launch(attn_int4_kernel<D, 5>, attn_int4_join_kernel<D, 5>, Sizes<D, 5>{});
+      case 1: return launch(dh, std::integral_constant<int, 1>{});
+      case 2: return launch(dh, std::integral_constant<int, 2>{});
+      case 3: return launch(dh, std::integral_constant<int, 3>{});
+      case 4: return launch(dh, std::integral_constant<int, 4>{});
+      default: return launch(dh, std::integral_constant<int, 5>{});
     }
   };
   LASER_TRY(kv->head_dim == 128 ? by_tiles(std::integral_constant<int, 128>{}) : by_tiles(std::integral_constant<int, 64>{}));

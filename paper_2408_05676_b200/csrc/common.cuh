@@ -2,6 +2,7 @@
 // per-device scratch buffers and small utilities.
 #pragma once
 #include <cuda_bf16.h>
+#include <atomic>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -92,6 +93,18 @@ inline cudaError_t launch_overlapped(void (*kernel)(P...), dim3 grid, unsigned t
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
+// Lets a kernel have that much dynamic shared memory (always the same amount of one kernel): once a device, not once a call.
+template <auto kKernel>
+inline cudaError_t allow_shared_memory(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && done.load(std::memory_order_relaxed) >> dev & 1)) return e;
+  e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+  return e;
 }
 #endif
 
