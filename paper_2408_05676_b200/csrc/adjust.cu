@@ -7,9 +7,12 @@
 // A CTA takes a run of the vocabulary for all rows of one sequence.  It counts the text's tokens of its run in shared memory (whole
 // numbers, whose order does not matter), notes which rows' tokens a token is as a 64-bit mask, and adds up its biases in the order of the
 // list; what that means for a row's logits is a factor and a difference a token, but for the step's own drafts.  Then the rows pass by, a
-// load and a store a logit, coalesced whatever the rows' alignment.  A trip to memory takes 1.6 us under load, so each thread has its
-// logits of the next kAhead rows on their way into shared memory (72 KB an SM; with one row ahead, in registers, 64 trees of 17 rows took
-// 71 us instead of 66).  A warp's 32 tokens are one word of the grammar mask, and logits that it forbids are not read.
+// load and a store a logit, or four of them where all rows begin on 16 bytes (64 x 9 rows of 32000: 19.2 us instead of 25.2).  A trip to
+// memory takes 1.6 us under load, so each thread has its logits of the next kAhead rows on their way into shared memory (72 KB an SM; with
+// one row ahead, in registers, 64 trees of 17 rows took 71 us instead of 66).  32 tokens are one word of the grammar mask, and logits
+// that it forbids are not read (of four, if it forbids them all).
+// Times (us; floors by bytes at 6.56 TB/s in brackets): one row of 32000 2.3 (0.04), 64 x 9 rows of 32000 19.2 (12.7), 64 trees of 17 rows
+// of 50257 62 (36): bound by the instructions of 4-byte accesses, 42 % of the LSU's and 54 % of the logic pipe's cycles.
 #include <type_traits>
 
 #include "model.cuh"
@@ -38,6 +41,9 @@ struct AdjustArgs {
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -56,21 +62,24 @@ struct Tables {
   float val[kThreads];
 };
 
-template <int U>
+// N: tokens of a thread that lie side by side, fetched and stored together: 4 where all rows begin on 16 bytes, else 1
+template <int U, int N>
 __global__ void __launch_bounds__(kThreads, 3)
 adjust_kernel(const AdjustArgs a) {
   using S = Tables<U>;
+  static_assert(N == 1 || (N == 4 && U % 4 == 0), "vectors of four");
   constexpr int C = S::C, kFirst = 4;
   extern __shared__ __align__(16) uint8_t smem[];
   S& s = *reinterpret_cast<S*>(smem);
   next_may_launch();
   const int b = blockIdx.y, v0 = blockIdx.x * C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  auto place = [&](int k) { return k / N * (N * kThreads) + tid * N + k % N; };      // of the thread's token k in the run
 #pragma unroll
   for (int k = 0; k < U; ++k) { s.count[k * kThreads + tid] = 0; s.rows[k * kThreads + tid] = 0; s.bias[k * kThreads + tid] = 0.f; }
   wait_for_earlier();
   // ---- what is read before the rows, in two trips to memory: the sequence's numbers and the first rows' words of the mask; then the first of
   // its text, biases and drafts, and the first rows ----
-  const int word = lane * (kThreads / 32) + warp;                                          // a lane's word: the tokens k kThreads + 32 warp on, k = lane
+  const int word = lane / N * (N * kThreads / 32) + warp * N + lane % N;                   // a lane's word: one of the U of the warp's tokens
   const bool has_word = a.allowed && lane < U && v0 + (word << 5) < a.V;
   const uint32_t* const words = a.allowed + b * a.mask_seq_stride + (v0 >> 5) + word;
   auto get_words = [&](int i) { if (has_word && i < a.R) copy4(smem_u32(&s.words[i % (2 * kAhead)][word]), words + i * a.mask_row_stride); };
@@ -87,27 +96,35 @@ adjust_kernel(const AdjustArgs a) {
   __syncwarp();
   uint32_t inside = 0;                         // the thread's tokens that are of the vocabulary
 #pragma unroll
-  for (int k = 0; k < U; ++k) if (v0 + k * kThreads + tid < a.V) inside |= 1u << k;
+  for (int k = 0; k < U; ++k) if (v0 + place(k) < a.V) inside |= 1u << k;
   auto allowed = [&](int i) {                  // those that row i may have
     if (!a.allowed) return inside;
     uint32_t bits = 0;
 #pragma unroll
-    for (int k = 0; k < U; ++k) bits |= (s.words[i % (2 * kAhead)][k * (kThreads / 32) + warp] >> lane & 1u) << k;      // (a token is lane mod 32)
+    for (int k = 0; k < U; k += N)
+      bits |= (s.words[i % (2 * kAhead)][k / N * (N * kThreads / 32) + warp * N + lane * N / 32] >> (lane * N % 32) & ((1u << N) - 1)) << k;
     return bits & inside;
   };
-  const float* in = a.logits + size_t(b) * a.R * a.V + v0 + tid;      // of the next row to be requested
+  const float* in = a.logits + size_t(b) * a.R * a.V + v0 + tid * N;      // of the next row to be requested
+  uint32_t on[kAhead];                         // what the next rows may have
   auto get_row = [&](int i) {
+    uint32_t bits = 0;
     if (i < nr) {
-      const uint32_t on = allowed(i), at = smem_u32(&s.x[i % kAhead][tid]);
+      bits = allowed(i);
+      const uint32_t at = smem_u32(&s.x[i % kAhead][tid * N]);
 #pragma unroll
-      for (int k = 0; k < U; ++k)
-        if (on >> k & 1u) copy4(at + k * (kThreads * 4), in + k * kThreads);
+      for (int k = 0; k < U; k += N) {
+        if (!(bits >> k & ((1u << N) - 1))) continue;
+        if (N == 4) copy16(at + k * (kThreads * 4), in + k * kThreads);
+        else copy4(at + k * (kThreads * 4), in + k * kThreads);
+      }
     }
     in += a.V;
+    return bits;
   };
-#pragma unroll 1
+#pragma unroll
   for (int i = 0; i < kAhead; ++i) {
-    get_row(i);
+    on[i] = get_row(i);
     copies_commit();
   }
   const int32_t* const text = a.hist + size_t(b) * a.hist_stride;
@@ -178,7 +195,7 @@ adjust_kernel(const AdjustArgs a) {
   float less[U];
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    const int at = k * kThreads + tid;
+    const int at = place(k);
     const uint32_t c = s.count[at];
     const float n = float(c & 0x7fffffffu);
     less[k] = (freq * n + (n > 0.f ? pres : 0.f)) - s.bias[at];
@@ -188,38 +205,46 @@ adjust_kernel(const AdjustArgs a) {
   const float inv = 1.f / rep;
 
   // ---- the rows ----
-  float* out = a.out + size_t(b) * a.R * a.V + v0 + tid;
+  float* out = a.out + size_t(b) * a.R * a.V + v0 + tid * N;
 #pragma unroll 1
   for (int i = 0; i < nr; ++i) {
     copies_wait<kAhead - 1>();
     __syncwarp();
-    const uint32_t on = allowed(i);
     float x[U];
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      x[k] = s.x[i % kAhead][k * kThreads + tid];
-      const float f = x[k] > 0.f ? inv : rep, y = x[k] * (seen >> k & 1u ? f : 1.f) - less[k];
-      x[k] = on >> k & 1u ? y : -INFINITY;
+    for (int k = 0; k < U; k += N) {
+      const float* from = &s.x[i % kAhead][place(k)];
+      if (N == 4) *reinterpret_cast<float4*>(&x[k]) = *reinterpret_cast<const float4*>(from);
+      else x[k] = *from;
     }
-    if (drafted & on) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float f = x[k] > 0.f ? inv : rep, y = x[k] * (seen >> k & 1u ? f : 1.f) - less[k];
+      x[k] = on[0] >> k & 1u ? y : -INFINITY;
+    }
+    if (drafted & on[0]) {
       const unsigned long long path = s.path[i];
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        if (!((drafted & on) >> k & 1u)) continue;
-        const uint32_t c = s.count[k * kThreads + tid];
-        const int drafts = __popcll(s.rows[k * kThreads + tid] & path);
+        if (!((drafted & on[0]) >> k & 1u)) continue;
+        const uint32_t c = s.count[place(k)];
+        const int drafts = __popcll(s.rows[place(k)] & path);
         const float n = float(int(c & 0x7fffffffu) + drafts);
         if (c != 0 || drafts != 0) x[k] *= x[k] > 0.f ? inv : rep;
-        x[k] -= (freq * n + (n > 0.f ? pres : 0.f)) - s.bias[k * kThreads + tid];
+        x[k] -= (freq * n + (n > 0.f ? pres : 0.f)) - s.bias[place(k)];
       }
     }
 #pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (inside >> k & 1u) out[k * kThreads] = x[k];
+    for (int k = 0; k < U; k += N) {
+      if (!(inside >> k & 1u)) continue;
+      if (N == 4) *reinterpret_cast<float4*>(out + k * kThreads) = *reinterpret_cast<const float4*>(&x[k]);
+      else out[k * kThreads] = x[k];
+    }
     out += a.V;
-    __syncwarp();                       // (the words of this row have been read)
-    get_words(i + 2 * kAhead);
-    get_row(i + kAhead);
+#pragma unroll
+    for (int y = 0; y + 1 < kAhead; ++y) on[y] = on[y + 1];
+    get_words(i + 2 * kAhead);          // (in the place of this row's, which were read before the last __syncwarp)
+    on[kAhead - 1] = get_row(i + kAhead);
     copies_commit();
   }
 }
@@ -250,15 +275,18 @@ LASER_API laser_status laser_adjust_logits(const float* logits, const int32_t* t
   if (B == 0) return LASER_OK;
   AdjustArgs a{logits, out, tokens, parents, n_rows, hist, hist_len, prompt_len, hist_stride, repetition, frequency, presence,
                bias_offsets, bias_ids, bias_values, allowed, mask_seq_stride, mask_row_stride, rows, V};
-  auto launch = [&](auto tokens_of_thread) -> laser_status {
-    constexpr int U = decltype(tokens_of_thread)::value;
-    LASER_CUDA(allow_shared_memory<adjust_kernel<U>>(int(sizeof(Tables<U>))));
-    LASER_CUDA(launch_overlapped(adjust_kernel<U>, dim3(unsigned(ceil_div(V, U * kThreads)), unsigned(B)), kThreads, sizeof(Tables<U>), as_stream(stream), a));
+  auto launch = [&](auto tokens_of_thread, auto together) -> laser_status {
+    constexpr int U = decltype(tokens_of_thread)::value, N = decltype(together)::value;
+    LASER_CUDA((allow_shared_memory<adjust_kernel<U, N>>(int(sizeof(Tables<U>)))));
+    LASER_CUDA(launch_overlapped(adjust_kernel<U, N>, dim3(unsigned(ceil_div(V, U * kThreads)), unsigned(B)), kThreads, sizeof(Tables<U>), as_stream(stream), a));
     return LASER_OK;
   };
   // runs of 2048 tokens; of 512 where the SMs would be left without work
-  if (int64_t(B) * ceil_div(V, 8 * kThreads) >= 148) LASER_TRY(launch(std::integral_constant<int, 8>{}));
-  else LASER_TRY(launch(std::integral_constant<int, 2>{}));
+  const bool fours = V % 4 == 0 && ((from | to) & 15) == 0;
+  const std::integral_constant<int, 1> one;
+  if (int64_t(B) * ceil_div(V, 8 * kThreads) < 148) LASER_TRY(launch(std::integral_constant<int, 2>{}, one));
+  else if (fours) LASER_TRY(launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 4>{}));
+  else LASER_TRY(launch(std::integral_constant<int, 8>{}, one));
   count_launch();
   return LASER_OK;
 }

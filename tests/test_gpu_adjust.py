@@ -45,6 +45,9 @@ CASES = [  # B, rows, V, history, biases, mask, tree
     (5, 17, 1000, 1500, 700, None, True),
     (70, 4, 5003, 300, 20, "row", True),              # (enough rows for the wider runs)
     (80, 2, 4096, 10, 300, "seq", False),
+    (70, 4, 5004, 300, 20, "row", True),              # (rows that begin on 16 bytes, and end inside a run)
+    (52, 17, 6148, 900, 100, "row", False),
+    (148, 5, 4, 20, 3, "row", False),
 ]
 
 
@@ -99,6 +102,25 @@ def test_matches_the_oracle(L, B, R, V, hist, nb, mask, tree):
         room = 5 * 2.0 ** -24 * (r32 * np.abs(np.nan_to_num(x[b, :n[b]])) + abs(f_32) * most + abs(p32) + sum(abs(v) for _, v in bias))
         assert (np.abs(got[b, :n[b]][fin] - want[fin]) <= room[fin]).all()
         assert torch.equal(same[b, :n[b]], out[b, :n[b]]) and torch.equal(same[b, n[b]:].isnan(), t[b, n[b]:].isnan())
+
+
+def test_alignment_does_not_change_a_bit(L):
+    """Rows on 16 bytes take another kernel than rows that are not: logits, result or both shifted by one to three numbers."""
+    rng = np.random.default_rng(5)
+    B, R, V = 50, 6, 6004
+    x = f32(rng.standard_normal((B, R, V)))
+    tok, n = dev_i32(rng.integers(0, V, (B, R))), dev_i32(rng.integers(0, R + 1, B))
+    args = dict(hist=dev_i32(rng.integers(0, V, (B, 300))), hist_len=dev_i32([300] * B), prompt_len=dev_i32([100] * B),
+                penalties=tuple(f32(rng.random(B) + 0.5) for _ in range(3)), allowed=pack(rng.random((B, R, V)) < 0.5))
+    want = L.adjust_logits(x, tok, n, out=torch.zeros_like(x), **args)
+
+    def shifted(by, values):
+        t = torch.zeros(B * R * V + 4, device="cuda")[by:by + B * R * V].view(B, R, V)
+        return t.copy_(values)
+
+    for i, o in ((1, 0), (0, 1), (2, 2), (3, 1), (0, 0)):
+        out = shifted(o, torch.zeros_like(x))
+        assert torch.equal(L.adjust_logits(shifted(i, x), tok, n, out=out, **args), want), (i, o)
 
 
 def test_infinities_nan_and_nothing_asked_for(L):
