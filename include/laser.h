@@ -302,7 +302,8 @@ laser_status laser_kv_append(laser_kv* kv, int32_t layer, const int32_t* seq_ids
  *        as they are
  * The work is divided evenly over the SMs whatever the lengths.  It keeps partial results in memory of
  * the cache's.  Asynchronous on `stream`.
- * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 1024, or tiles of rows x pages beyond 2^31 a sequence); on the device as above. */
+ * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 1024, or tiles of up to 40
+ * rows x pages beyond 2^31 for a sequence or, of all, for an SM); on the device as above. */
 laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int32_t* seq_ids, const int32_t* parents,
                                const int32_t* n_rows, int32_t B, int32_t rows, const void* q, int64_t q_stride,
                                void* out, int64_t out_stride, void* stream);

@@ -227,7 +227,7 @@ attn_int4_kernel(const AttnArgs a) {
     __syncthreads();
   }
   if (a.row_ctx) wait_for_earlier();
-  // (a CTA's share is below 2^31 blocks: the cache has no more than that, and a call no more tiles than that allows)
+  // (below 2^31: launch_attention sees to it)
   constexpr int kLeast = 2 / S;        // blocks of a team: two pages are in flight together anyway
   const int per_cta = max(total <= 0xffffffffll ? int((unsigned(total) + gridDim.x - 1) / gridDim.x) : int((total + gridDim.x - 1) / gridDim.x), 2 * kLeast);
   const long long c0 = (long long)per_cta * blockIdx.x;
@@ -750,8 +750,9 @@ laser_status launch_attention(const laser_kv* kv, AttnArgs a, cudaStream_t strea
   const int64_t rows = int64_t(a.Rs) * a.G;
   const int nt = row_tiles(int(std::min<int64_t>(rows, 1 << 28)));
   const int64_t units = a.Hkv * ceil_div(rows, int64_t(8 * nt));          // of a sequence, at most
-  if (units * kv->pages_per_seq > INT32_MAX) {
-    set_error("%lld row tiles a sequence over caches of %d pages are too many for one call", (long long)units, kv->pages_per_seq);
+  // (a sequence's blocks, and a CTA's share of them all, are counted in 32 bits)
+  if (units * kv->pages_per_seq > INT32_MAX || units * kv->pages_per_seq * a.B / kv->attn_ctas >= INT32_MAX) {
+    set_error("%lld row tiles a sequence (of %d) over caches of %d pages are too many for one call", (long long)units, a.B, kv->pages_per_seq);
     return LASER_ERR_CAPACITY;
   }
   a.vec_out = (reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.ldo * 2)) % 16 == 0;

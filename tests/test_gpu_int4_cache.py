@@ -478,6 +478,16 @@ def test_refusals(L):
         refused(-1, lambda: L.kv_create_int4(usual, slots, pages))
 
 
+def test_more_work_than_32_bits_count_is_refused(L):
+    kv = make(L, 1, 1, 64, 1, 16384)
+    ids, n, x = dev_i32([0] * 160), dev_i32([0] * 160), torch.zeros(64, dtype=torch.bfloat16, device="cuda")
+    call = lambda B, rows: L.lib.laser_attend_int4(kv.handle, 0, ids.data_ptr(), None, n.data_ptr(), B, rows, x.data_ptr(), 64, x.data_ptr(), 64, None)
+    assert call(160, 40 * 131071) == -4             # 160 x 131071 tiles x 16384 pages: 2.3e9 an SM
+    assert call(1, 40 * 131073) == -4
+    assert call(160, 1000) == 0                     # (no row is active)
+    L.kv_check(kv)
+
+
 # ---- together ----------------------------------------------------------------------------------------------------
 
 def test_append_and_attend_on_another_stream_and_in_a_graph(L):
