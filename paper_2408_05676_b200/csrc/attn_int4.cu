@@ -609,21 +609,25 @@ attn_int4_kernel(const AttnArgs a) {
 #pragma unroll 1
   for (int y = tid; y < cuts * TM; y += W * 32) {
     const Cut& c = s_cut[y / TM];
-    const int row = y % TM;
+    const int row = y % TM, first = c.first, last = c.last, at_end = c.early ? last : -1;
+    float2 ml[T];
     float m = -INFINITY, l = 0.f;
-    for (int x = c.first; x <= c.last; ++x) m = fmaxf(m, s_ml[x][c.early && x == c.last ? 0 : 1][row].x);
+#pragma unroll
+    for (int x = 0; x < T; ++x) {
+      ml[x] = x >= first && x <= last ? s_ml[x][x == at_end ? 0 : 1][row] : make_float2(-INFINITY, 0.f);
+      m = fmaxf(m, ml[x].x);
+    }
     const float zero = m == -INFINITY ? 0.f : m;
-    for (int x = c.first; x <= c.last; ++x) {
-      float2& ml = s_ml[x][c.early && x == c.last ? 0 : 1][row];
-      ml.x = ex2(ml.x - zero);
-      l += ml.y * ml.x;
+#pragma unroll
+    for (int x = 0; x < T; ++x) {
+      ml[x].x = ex2(ml[x].x - zero);
+      l += ml[x].y * ml[x].x;
     }
-    if (c.open) {
-      __stcg(reinterpret_cast<float2*>(record(c) + Z::kOBytes / 4) + row, make_float2(m, l));
-    } else {
-      const float inv = 1.f / l;
-      for (int x = c.first; x <= c.last; ++x) s_ml[x][c.early && x == c.last ? 0 : 1][row].x *= inv;
-    }
+    if (c.open) __stcg(reinterpret_cast<float2*>(record(c) + Z::kOBytes / 4) + row, make_float2(m, l));
+    const float by = c.open ? 1.f : 1.f / l;
+#pragma unroll
+    for (int x = 0; x < T; ++x)
+      if (x >= first && x <= last) s_ml[x][x == at_end ? 0 : 1][row].x = ml[x].x * by;
   }
   __syncthreads();
 #pragma unroll 1
