@@ -22,8 +22,8 @@
 // Where a unit is cut, the pieces (m, sum, O in fp32) meet twice, in the order of the pages both times: the teams' in their CTA after its
 // last page, the CTAs' in a kernel that follows.
 //
-// Times (us; floors by bytes at 6.56 TB/s in brackets): 32 heads of 128, 9 rows over one text of 512 tokens 9.3 (0.4), over 16 of 256 to 768
-// 21.7 (6.7); 40 heads, trees of 17 rows over 64 texts of 256 to 1024 122 (42); 32 heads of 8 kv heads, one row over 64 texts of 4096 to 8192
+// Times (us; floors by bytes at 6.56 TB/s in brackets): 32 heads of 128, 9 rows over one text of 512 tokens 9.1 (0.4), over 16 of 256 to 768
+// 21.4 (6.7); 40 heads, trees of 17 rows over 64 texts of 256 to 1024 122 (42); 32 heads of 8 kv heads, one row over 64 texts of 4096 to 8192
 // 101 (77), 9 rows over one of 65536 52 (13).
 #include <algorithm>
 #include <cmath>

@@ -61,30 +61,33 @@ __device__ __forceinline__ Q4Scale q4_scale(const float (&x)[4]) {
   q.z = bf16_bits(__fsub_rn(lo, 16.f * bf16_value(q.s)));
   return q;
 }
-// The codes of four values.  The quotient is the rounded one's neighbour at most (31 x 2^-22); where that could decide between two codes
-// the division itself is made.
-__device__ __forceinline__ void q4_codes(const float (&x)[4], const Q4Scale& q, uint32_t (&code)[4]) {
+// 16 + the codes of four values.  The quotient is the rounded one's neighbour at most (31 x 2^-22); where that could decide between two
+// codes the division itself is made.  Rounded by adding 1.5 x 2^23 (quotients are below 2^20: a group's range is a few of its largest
+// magnitude's 2^-24 at least, z is off by 2^-9 of it): conversions have a quarter of the other instructions' rate, and with three a value
+// they took half of the time of an append.
+__device__ __forceinline__ void q4_codes(const float (&x)[4], const Q4Scale& q, float (&at)[4]) {
+  constexpr float kRound = 12582912.f;
   const float s = bf16_value(q.s), z = bf16_value(q.z);
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
   bool clear = true;
-  float v[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    v[u] = __fsub_rn(x[u], z) * inv;
-    clear = clear && fabsf(fabsf(v[u] - rintf(v[u])) - 0.5f) > 4e-5f;
+    const float v = __fmul_rn(__fsub_rn(x[u], z), inv);
+    at[u] = __fsub_rn(__fadd_rn(v, kRound), kRound);
+    clear = clear && fabsf(__fsub_rn(v, at[u])) < 0.5f - 4e-5f;
   }
   if (!clear) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = __fdiv_rn(__fsub_rn(x[u], z), s);
+    for (int u = 0; u < 4; ++u) at[u] = __fsub_rn(__fadd_rn(__fdiv_rn(__fsub_rn(x[u], z), s), kRound), kRound);
   }
 #pragma unroll
-  for (int u = 0; u < 4; ++u) code[u] = q.s == 0 ? 0u : uint32_t(fminf(fmaxf(rintf(v[u]) - 16.f, 0.f), 15.f));
+  for (int u = 0; u < 4; ++u) at[u] = q.s == 0 ? 16.f : fminf(fmaxf(at[u], 16.f), 31.f);
 }
+// two codes c, d given as 16 + c, 16 + d: c | d << 4 in the low byte, nothing in the next
+__device__ __forceinline__ uint32_t q4_two(float c, float d) { return __float_as_uint(__fmaf_rn(16.f, d, c + (8388608.f - 272.f))); }
 // (the product is exact: eight and five bits)
-__device__ __forceinline__ uint32_t q4_held(uint32_t code, const Q4Scale& q) {
-  return bf16_bits(__fmaf_rn(bf16_value(q.s), float(16 + int(code)), bf16_value(q.z)));
-}
+__device__ __forceinline__ float q4_held(float at, const Q4Scale& q) { return __fmaf_rn(bf16_value(q.s), at, bf16_value(q.z)); }
 #endif
 
 }  // namespace laser

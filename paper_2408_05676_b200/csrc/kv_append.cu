@@ -4,7 +4,12 @@
 // Row i of sequence b sits at position len + depth(i) (chain: len + i) and goes to slot len + i.  The pair (x_j, x_{j + dh/2}) turns by
 // position x theta^(-2j / dh); angles in 64 bits, since fp32 products are off by 1e-2 rad at position 1e5, the rotation itself in fp32.
 // A block takes one row and a share of its heads, so that a row's sines are worked out once per block; a lane holds four features
-// (8 or 16 bytes a load), head_dim / 4 lanes a head, the rotation's partner and a group's extremes come by shuffles.
+// (8 or 16 bytes a load), head_dim / 4 lanes a head, the rotation's partner and a group's extremes come by shuffles.  (Eight features a lane, with
+// no shuffle for the rotation, took twice the code and 80 registers: 128 us instead of 72 for the prompts below.)
+//
+// Times into a 4-bit cache (us; floors by bytes at 6.56 TB/s in brackets): one row of 4 heads of 64 4.3, 16 x 9 rows of 32 heads of 128 7.2 (0.7), both
+// two dependent trips to memory and the sines; 64 trees of 17 rows of 40 heads in fp32 16.8 (8.7); prompts of 10 thousand rows of 32 heads, 8 kv heads,
+// 63 (32): bound by instructions, of which codes of keys and values take half (queries alone: 33 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -182,24 +187,24 @@ kv_append_kernel(const AppendArgs a) {
         } else {
           q4_finite(y);
           const Q4Scale sc = q4_scale(y);
-          uint32_t code[4];
-          q4_codes(y, sc, code);
+          float at[4];
+          q4_codes(y, sc, at);
           uint8_t* blk = page + h * q4_block_bytes(DH);
           if (kKind == 1) {
-            uint32_t kw = code[0] << 3 | code[1] << 19 | code[2] << 7 | code[3] << 23;
+            uint32_t kw = __byte_perm(q4_two(at[0], at[2]), q4_two(at[1], at[3]), 0x5410) << 3;      // codes at bits 3, 19, 7, 23
             if (l & 1) kw = __funnelshift_l(kw, kw, 8);
             kw |= __shfl_xor_sync(0xffffffffu, kw, 1);
             if (live && !(l & 1)) *reinterpret_cast<uint32_t*>(blk + q4_k_codes(DH, t, l >> 1)) = kw;
             if (live && !(l & 7)) *reinterpret_cast<uint32_t*>(blk + q4_k_scale(DH, t, l >> 3)) = sc.s | sc.z << 16;
           } else if (live) {
-            *reinterpret_cast<uint16_t*>(blk + q4_v_codes(DH, t, l)) = uint16_t(code[0] | code[1] << 4 | code[2] << 8 | code[3] << 12);
+            *reinterpret_cast<uint16_t*>(blk + q4_v_codes(DH, t, l)) = uint16_t(__byte_perm(q4_two(at[0], at[1]), q4_two(at[2], at[3]), 0x0040));
             if (!(l & 7)) {
               uint8_t* p = blk + q4_v_scale(DH, t, l >> 3);
               *reinterpret_cast<uint16_t*>(p) = uint16_t(sc.s);
               *reinterpret_cast<uint16_t*>(p + 4) = uint16_t(sc.z);
             }
           }
-          if (to) held = make_uint2(q4_held(code[0], sc) | q4_held(code[1], sc) << 16, q4_held(code[2], sc) | q4_held(code[3], sc) << 16);
+          if (to) held = make_uint2(two_bf16(q4_held(at[0], sc), q4_held(at[1], sc)), two_bf16(q4_held(at[2], sc), q4_held(at[3], sc)));
         }
         if (to && live) *reinterpret_cast<uint2*>(to + (size_t(r) * count + h) * DH + 4 * l) = held;
       }
@@ -234,9 +239,9 @@ __global__ void export_q4_kernel(const uint8_t* __restrict__ pages, const int32_
       w = __funnelshift_r(w, w, 3 + 8 * (c4 & 1));           // features at bits 0, 16, 4, 20
       codes = (w & 15u) | (w >> 16 & 15u) << 4 | (w >> 4 & 15u) << 8 | (w >> 20 & 15u) << 12;
     }
-    uint32_t held[4];
-    for (int u = 0; u < 4; ++u) held[u] = q4_held(codes >> (4 * u) & 15u, sc);
-    *reinterpret_cast<uint2*>((is_v ? v : k) + (tok * Hkv + h) * dh + 4 * c4) = make_uint2(held[0] | held[1] << 16, held[2] | held[3] << 16);
+    float held[4];
+    for (int u = 0; u < 4; ++u) held[u] = q4_held(float(16 + int(codes >> (4 * u) & 15u)), sc);
+    *reinterpret_cast<uint2*>((is_v ? v : k) + (tok * Hkv + h) * dh + 4 * c4) = make_uint2(two_bf16(held[0], held[1]), two_bf16(held[2], held[3]));
   }
 }
 
