@@ -150,6 +150,37 @@ def test_append_matches_the_oracle(L, heads, kv_heads, dim, lens, n_rows, rows, 
     assert flips <= max(1, total // 10000), (flips, total)
 
 
+def test_codes_of_values_at_borders_and_a_few_ulps_apart(L):
+    """fp32 values are stored to the bit as the oracle has it: halfway between two codes and next to that, ranges of a few of the values'
+    last places (the zero is then far from them, in steps), tiny steps, the largest magnitudes."""
+    rng = np.random.default_rng(17)
+    n, dim = 240, 128
+    kv = make(L, 1, 1, dim, 1, 16)
+    x = np.zeros((n, dim), np.float32)
+    for i in range(n):
+        kind, g = i % 6, rng.integers(0, 16, dim).astype(np.float64)
+        g[::32], g[1::32] = 0, 15
+        step = 2.0 ** int(rng.integers(-90, 100))
+        if kind < 2:                                         # c + 1/2, and a last place beside it
+            v = ((g + 0.5 * (g % 15 != 0)) * step).astype(np.float32)
+            x[i] = v if kind == 0 else np.nextafter(v, np.float32(rng.choice([-1, 1]) * np.inf), dtype=np.float32)
+        elif kind == 2:                                      # a few last places of a large number
+            x[i] = (np.float32(step) * np.float32(rng.uniform(1, 2))).view(np.uint32).__add__(rng.integers(0, rng.choice([2, 3, 40, 5000]), dim)).astype(np.uint32).view(np.float32)
+        elif kind == 3:                                      # steps near the least one
+            x[i] = (rng.uniform(-8, 8, dim) * 2.0 ** -100 * 2.0 ** rng.integers(-3, 3)).astype(np.float32)
+        elif kind == 4:
+            x[i] = np.clip(rng.standard_normal(dim) * 2.0 ** 125, -3.4e38, 3.4e38).astype(np.float32)
+        else:
+            x[i] = (rng.standard_normal(dim) * 1e-3 + rng.choice([-1, 1]) * 10.0 ** rng.integers(0, 6)).astype(np.float32)
+    t = torch.as_tensor(x, device="cuda").view(1, n, dim)
+    vo = torch.empty(1, n, 1, dim, dtype=torch.bfloat16, device="cuda")
+    L.kv_append(kv, 0, dev_i32([0]), dev_i32([n]), t, t, v_out=vo)
+    L.kv_check(kv)
+    want = Q.held(x)
+    assert (f64(vo)[0, :, 0] == want).all()
+    assert (held_rows(L, kv, 0, 0, n)[1][:, 0] == want).all()
+
+
 def test_append_far_positions_and_unaligned_rows(L):
     """Angles of positions beyond 10^5 in 64 bits; rows whose alignment allows no wide loads give the same."""
     kv = make(L, 2, 1, 64, 1, 16384)
