@@ -47,14 +47,17 @@ struct Join { int b, hk, row0, rows, count; };
 
 template <int DH, int NT>
 struct Sizes {
-  // A team is a warp, or two that take a page each of every two and half of the features each
+  // A team is a warp, or two that take a page each of every two and half of the features each (one row over long texts: 100 us alone, 112 in
+  // twos; 36 rows: 66 alone, 52 in twos)
   static constexpr int kTeam = NT == 1 ? 1 : 2;
   static constexpr int kRegsO = NT * DH / 4 / kTeam;     // O registers of a lane
-  static constexpr int kWarps = NT == 1 ? 16 : kRegsO <= 48 ? 12 : 8;      // as many as the registers allow without spills
+  // as many warps as the registers allow without spills (heads of 64, 9 rows: 55 us with 16, 58 with 12, 71 with 8; of 128, 17 rows: 157 with 16
+  // and spills, 121 with 12, 137 with 8; 36 rows: 65 with 12 and spills, 52 with 8)
+  static constexpr int kWarps = NT == 1 || kRegsO <= 24 ? 16 : kRegsO <= 48 ? 12 : 8;
   static constexpr int kTeams = kWarps / kTeam;
   static constexpr int kRows = 8 * NT;
   static constexpr int kBlock = q4_block_bytes(DH);      // bytes of a page and head
-  static constexpr int kStages = DH == 64 ? 6 : kTeam == 1 ? 4 : 3;      // of a warp's ring
+  static constexpr int kStages = kTeam == 1 ? 4 : 3;     // of a warp's ring (one more: no change)
   static constexpr bool kQInSmem = NT > 1;               // each lane's share of Q is put by and read again for every page
   static constexpr int kQBytes = kQInSmem ? NT * DH / 8 * 4 * 32 : 0;
   static constexpr int kPBytes = kTeam == 1 ? 0 : NT * 2 * 256;          // P of two pages
