@@ -235,8 +235,9 @@ laser_status laser_kv_create(const laser_model* m, int32_t max_seqs, int64_t n_p
 laser_status laser_kv_free(laser_kv* kv);
 /* The same in 4 bits: 5 bits a value with its scales, 0.31 of the bf16 cache's memory and traffic.
  * Per token, head and group of 32 features there are codes 0 .. 15, a scale s and a zero z in bf16:
- *   s = bf16((max - min) / 15), 0 where that is below 2^-100;  z = bf16(min - 16 s)
+ *   s = bf16((max - min) * (1 / 15)), 0 where that is below 2^-100;  z = bf16(min - 16 s)
  *   code = rint((x - z) / s) - 16, clamped to 0 .. 15 (0 where s = 0), stands for bf16(s (16 + code) + z)
+ * each operation in fp32, the quotient (x - z) / s rounded as a division's.
  * (NaN is stored as 0 and magnitudes above 2^124 as 2^124: the cache holds finite numbers alone).
  * Every call that takes a cache takes either form: laser_verify_step, _tree, laser_verify_accept and
  * laser_generate write and read it, laser_kv_import rounds to it, laser_kv_export gives the bf16

@@ -1,7 +1,7 @@
 """Oracle of the 4-bit cache and of the operators on it.  Test infrastructure only (see the package docstring).
 
 Format: per token, head and group of 32 features, codes 0 .. 15 with a scale s and a zero z in bf16,
-    s = bf16((max - min) / 15), 0 where that is below 2^-100;  z = bf16(min - 16 s)
+    s = bf16((max - min) * (1 / 15)), 0 where that is below 2^-100;  z = bf16(min - 16 s)
     code = rint((x - z) / s) - 16, clamped to 0 .. 15 (0 where s = 0);  held: bf16(s (16 + code) + z)
 after NaN -> 0 and clamping to +-2^124.  The inputs are fp32 numbers and the steps before z's and s's rounding to bf16, and the
 quotient before rint, are rounded to fp32, as the definition of a code at a border; everything else is exact in fp64.
@@ -26,7 +26,7 @@ def quantise(x):
     x = np.clip(np.where(np.isnan(x), np.float32(0), x), np.float32(-TOP), np.float32(TOP))
     x = x.reshape(x.shape[:-1] + (-1, GROUP))
     lo, hi = x.min(-1), x.max(-1)
-    s = bf16((hi - lo) / np.float32(15))
+    s = bf16((hi - lo) * (np.float32(1) / np.float32(15)))
     s = np.where(s < LEAST, 0.0, s)
     z = bf16(lo - np.float32(16) * s.astype(np.float32))
     safe = np.where(s > 0, s, 1.0).astype(np.float32)[..., None]

@@ -1,10 +1,10 @@
 // The 4-bit form of the paged cache.  Per token, head and group of 32 features: codes 0 .. 15, a scale s and a zero z in bf16.  With
-// lo and hi the group's extremes, s = bf16((hi - lo) / 15), z = bf16(lo - 16 s), code = rint((x - z) / s) - 16 clamped to 0 .. 15, and
+// lo and hi the group's extremes, s = bf16((hi - lo) x 1/15), z = bf16(lo - 16 s), code = rint((x - z) / s) - 16 clamped to 0 .. 15, and
 // a code stands for bf16(s (16 + code) + z), rounded once.  16 + code is what the attention kernel finds most easily: 0x4180 | code << 3
 // as bf16, so that two codes become two values by one logic instruction and one packed multiply-add.  Everything held is finite: NaN is
 // stored as 0 and magnitudes above 2^124 as 2^124, so that a masked token cannot spoil a row (weight 0 times its value is 0).
 //
-// A page and kv head is one block of 20 head_dim bytes, a single bulk copy:
+// A page and kv head is one block of 20 head_dim bytes:
 //   K codes   [16 tokens][head_dim / 8 words]   word: features 8i .. 8i+7, feature c at bits 3 + 4 (c / 2) + 16 (c % 2) on (mod 32): rotating
 //                                               right by 4e leaves features 2e and 2e+1 at bits 3 .. 6 of the two halves
 //   K scales  [16 tokens][head_dim / 32]        s | z << 16
@@ -56,7 +56,7 @@ __device__ __forceinline__ Q4Scale q4_scale(const float (&x)[4]) {
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
   Q4Scale q;
-  q.s = bf16_bits(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
+  q.s = bf16_bits(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f));      // (the step is part of the format: one product, not a division)
   if (bf16_value(q.s) < kQ4Least) q.s = 0;
   q.z = bf16_bits(__fsub_rn(lo, 16.f * bf16_value(q.s)));
   return q;

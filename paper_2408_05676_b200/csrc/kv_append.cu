@@ -7,9 +7,9 @@
 // (8 or 16 bytes a load), head_dim / 4 lanes a head, the rotation's partner and a group's extremes come by shuffles.  (Eight features a lane, with
 // no shuffle for the rotation, took twice the code and 80 registers: 128 us instead of 72 for the prompts below.)
 //
-// Times into a 4-bit cache (us; floors by bytes at 6.56 TB/s in brackets): one row of 4 heads of 64 4.3, 16 x 9 rows of 32 heads of 128 7.2 (0.7), both
-// two dependent trips to memory and the sines; 64 trees of 17 rows of 40 heads in fp32 16.8 (8.7); prompts of 10 thousand rows of 32 heads, 8 kv heads,
-// 63 (32): bound by instructions, of which codes of keys and values take half (queries alone: 33 us).
+// Times into a 4-bit cache (us; floors by bytes at 6.56 TB/s in brackets): one row of 4 heads of 64 4.3, 16 x 9 rows of 32 heads of 128 7.1 (0.7), both
+// two dependent trips to memory and the sines; 64 trees of 17 rows of 40 heads in fp32 16.5 (8.7); prompts of 10 thousand rows of 32 heads, 8 kv heads,
+// 62 (32): bound by instructions, of which codes of keys and values take half (queries alone: 33 us).
 #include <algorithm>
 #include <type_traits>
 
