@@ -632,6 +632,29 @@ def test_verify_step_on_a_4bit_cache(L, over, tree):
                 assert (np.abs(held[l][b][y][lens[b]:] - x) <= room).all()
 
 
+def test_a_cache_serves_models_with_other_query_heads(L):
+    """A cache is shaped by keys and values: whichever model made it, a step takes its heads from the model that runs."""
+    cfgs = [synth.model_cfg("tiny", d_model=256, n_heads=h, n_kv_heads=2, head_dim=64) for h in (4, 10)]
+    models = [L.model_create(c, weights_to(synth.make_weights(c, seed=7), "cuda"), max_batch=2) for c in cfgs]
+    R = cfgs[0]["max_draft"] + 1
+    rng = np.random.default_rng(23)
+    tokens, n, ids = dev_i32(rng.integers(0, cfgs[0]["vocab"], (2, R))), dev_i32([R, 4]), dev_i32([0, 1])
+    x = [bf(rng.standard_normal((40, 128))) for _ in range(2)]
+    for m in models:
+        got = []
+        for maker in models:
+            kv = L.kv_create_int4(maker, 2, 8)
+            for l in range(cfgs[0]["n_layers"]):
+                for b in range(2):
+                    L.kv_import(kv, b, l, 0, x[0], x[1])
+            L.kv_set_len(kv, [0, 1], [40, 23])
+            logits = L.verify_step(m, kv, ids, tokens, n)
+            L.check(m)
+            got.append((logits[0], logits[1, :4], *held_rows(L, kv, 0, 0, 40 + R)))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert all((p == q).all() for p, q in zip(got[0][2:], got[1][2:])) and torch.isfinite(got[0][0]).all()
+
+
 def test_tree_commit_moves_codes(L):
     """laser_kv_compact_path on a 4-bit cache: accepted rows move as they are, across pages, in every layer."""
     kv = make(L, 4, 2, 128, 3, 6, layers=2)
