@@ -418,6 +418,13 @@ LASER_API laser_status laser_kv_free(laser_kv* kv) {
   return LASER_OK;
 }
 
+// cudaMemset returns before it is done, and streams made without it do not wait for the default stream: what a call has zeroed is
+// handed out when it is.
+static laser_status memsets_done() {
+  LASER_CUDA(cudaStreamSynchronize(nullptr));
+  return LASER_OK;
+}
+
 // The parts that caches of both forms have.
 static laser_status kv_open(const laser_model* m, int32_t max_seqs, int64_t n_pages, laser_kv* kv) {
   kv->n_layers = m->cfg.n_layers; kv->n_kv_heads = m->cfg.n_kv_heads; kv->head_dim = m->cfg.head_dim; kv->n_heads = m->cfg.n_heads;
@@ -454,6 +461,7 @@ LASER_API laser_status laser_kv_create(const laser_model* m, int32_t max_seqs, i
     LASER_TRY(encode_bf16_2d(&kv->pages_map, kv->pages, map_rows, uint64_t(kv->head_dim), 16));
     kv->has_pages_map = true;
   }
+  LASER_TRY(memsets_done());
   guard.p = nullptr;
   *out = kv;
   return LASER_OK;
@@ -475,6 +483,7 @@ LASER_API laser_status laser_kv_create_int4(laser_model* m, int32_t max_seqs, in
   LASER_CUDA(cudaGetDevice(&dev));
   LASER_CUDA(cudaDeviceGetAttribute(&kv->attn_ctas, cudaDevAttrMultiProcessorCount, dev));
   LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->attn_part), attention_int4_part_floats(kv->head_dim, kv->attn_ctas) * sizeof(float)));
+  LASER_TRY(memsets_done());
   guard.p = nullptr;
   *out = kv;
   return LASER_OK;
