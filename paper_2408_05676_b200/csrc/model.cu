@@ -281,8 +281,16 @@ laser_status fuse_rows(laser_model* m, const void* const* pieces, const size_t* 
   return LASER_OK;
 }
 
-// Rows for a layer's projections, which a step over a 4-bit cache keeps in fp32 until they are rotated and stored.
-laser_status qkv_rows(laser_model* m) { return m->qkv ? LASER_OK : model_alloc(m, &m->qkv, size_t(m->R_cap) * m->dqkv); }
+// Rows for a layer's projections, which a step over a 4-bit cache keeps in fp32 until they are rotated and stored.  Not zeroed: the projection
+// writes every row that is read, and a memset would not be in the order of the step's stream.
+laser_status qkv_rows(laser_model* m) {
+  if (m->qkv) return LASER_OK;
+  float* rows = nullptr;
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&rows), size_t(m->R_cap) * m->dqkv * sizeof(float)));
+  m->owned.push_back(rows);
+  m->qkv = rows;
+  return LASER_OK;
+}
 
 }  // namespace
 }  // namespace laser

@@ -33,3 +33,25 @@ def test_a_new_cache_is_empty_before_the_call_returns(L, int4):
     assert done
     k, v = L.kv_export(kv, 0, 0, (pages - 10) * 16, 160)
     assert torch.equal(k, v) and (k.float() - x.float()).abs().max() <= (0.5 if int4 else 0)
+
+
+def test_a_model_that_first_meets_a_4bit_cache_in_a_step(L):
+    """Its rows for projections are made in the step: nothing that is still to come touches them."""
+    cfg = synth.model_cfg("tiny", n_layers=12, d_model=256, n_heads=32, n_kv_heads=8, head_dim=128, d_ffn=256, vocab=64, max_draft=8)
+    W = weights_to(synth.make_weights(cfg, seed=3), "cuda")
+    maker = L.model_create(cfg, W, max_batch=8)
+    ids, n = dev_i32(range(8)), dev_i32([9] * 8)
+    tokens = dev_i32([synth.make_prompt(9, cfg["vocab"], s) for s in range(8)])
+    kv = L.kv_create_int4(maker, 8, 8)
+    want = L.verify_step(maker, kv, ids, tokens, n)
+    stream = torch.cuda.Stream(priority=-1)
+    for busy in (2_000_000, 6_000_000, 10_000_000):        # clocks for which the default stream has work that it began before
+        other = L.model_create(cfg, W, max_batch=2048)      # (18432 rows of 6144 numbers)
+        logits = [torch.empty_like(want) for _ in range(60)]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(busy)
+        for x in logits:
+            L.verify_step(other, kv, ids, tokens, n, logits=x, stream=stream)
+        torch.cuda.synchronize()
+        L.check(other)
+        assert all(torch.equal(x, want) for x in logits)
