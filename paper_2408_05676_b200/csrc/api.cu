@@ -101,6 +101,7 @@ laser_status scratch_get(int slot, size_t bytes, void** out) {
     size_t want = (bytes + 255) & ~size_t(255);
     LASER_CUDA(device_malloc(&s.ptr, want));
     LASER_CUDA(cudaMemset(s.ptr, 0, want));
+    LASER_CUDA(cudaStreamSynchronize(nullptr));      // (the caller's stream need not wait for the default one)
     s.bytes = want;
   }
   *out = s.ptr;

@@ -261,6 +261,13 @@ laser_status model_alloc(laser_model* m, T** p, size_t count) {
   return LASER_OK;
 }
 
+// cudaMemset, like a copy on the device, returns before it is done, and streams may be made that do not wait for the default stream: what a
+// call has written there is handed out when it is done.
+laser_status memsets_done() {
+  LASER_CUDA(cudaStreamSynchronize(nullptr));
+  return LASER_OK;
+}
+
 // Returns `first` if the pieces are adjacent in memory, else a fused device copy.
 laser_status fuse_rows(laser_model* m, const void* const* pieces, const size_t* elems, int n,
                        const bf16** out) {
@@ -413,6 +420,7 @@ LASER_API laser_status laser_model_create(const laser_model_cfg* cfg, const lase
   LASER_TRY(model_alloc(m, &slab, total));
   size_t off = 0;
   for (const Part& x : parts) { *x.p = slab + off; off += (x.bytes + 255) & ~size_t(255); }
+  LASER_TRY(memsets_done());
   guard.p = nullptr;
   *out = m;
   return LASER_OK;
@@ -423,13 +431,6 @@ LASER_API laser_status laser_kv_free(laser_kv* kv) {
   cudaFree(kv->pages); cudaFree(kv->pages4); cudaFree(kv->page_table); cudaFree(kv->seq_len);
   cudaFree(kv->inv_freq); cudaFree(kv->status); cudaFree(kv->attn_part);
   delete kv;
-  return LASER_OK;
-}
-
-// cudaMemset returns before it is done, and streams made without it do not wait for the default stream: what a call has zeroed is
-// handed out when it is.
-static laser_status memsets_done() {
-  LASER_CUDA(cudaStreamSynchronize(nullptr));
   return LASER_OK;
 }
 

@@ -35,6 +35,27 @@ def test_a_new_cache_is_empty_before_the_call_returns(L, int4):
     assert torch.equal(k, v) and (k.float() - x.float()).abs().max() <= (0.5 if int4 else 0)
 
 
+def test_a_new_model_is_ready_before_the_call_returns(L):
+    """A workspace of gigabytes to be zeroed; a step runs at once."""
+    cfg = synth.model_cfg("tiny", n_layers=2, d_model=512, d_ffn=65536, vocab=64, max_draft=63)
+    W = weights_to(synth.make_weights(cfg, seed=3), "cuda")
+    ids, n = dev_i32([0]), dev_i32([64])
+    tokens = dev_i32([synth.make_prompt(64, cfg["vocab"], 1)])
+    stream = torch.cuda.Stream(priority=-1)
+    first = L.model_create(cfg, W, max_batch=512)
+    kv = L.kv_create(first, 1, 8)
+    torch.cuda.synchronize()
+    want = L.verify_step(first, kv, ids, tokens, n)
+    logits = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    m = L.model_create(cfg, W, max_batch=512)
+    assert torch.cuda.default_stream().query()
+    L.verify_step(m, kv, ids, tokens, n, logits=logits, stream=stream)
+    torch.cuda.synchronize()
+    L.check(m)
+    assert torch.equal(logits, want)
+
+
 def test_a_model_that_first_meets_a_4bit_cache_in_a_step(L):
     """Its rows for projections are made in the step: nothing that is still to come touches them."""
     cfg = synth.model_cfg("tiny", n_layers=12, d_model=256, n_heads=32, n_kv_heads=8, head_dim=128, d_ffn=256, vocab=64, max_draft=8)
