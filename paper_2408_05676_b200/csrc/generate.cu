@@ -247,6 +247,10 @@ LASER_API laser_status laser_generate(laser_model* m, laser_kv* kv, const laser_
   LASER_REQUIRE(pool == nullptr || (p->K >= 1 && p->n_max >= 1 && p->n_max <= 8), "drafting needs K >= 1 and n_max in [1, 8]");
   LASER_REQUIRE(!p->temp_branches || pool != nullptr, "temporary branches are drafted beside a pool");
   LASER_REQUIRE(!p->tree || pool != nullptr, "tree drafting needs a pool");
+  if (kv->pages4 && B > attention_int4_max_groups()) {
+    set_error("B = %d sequences over a 4-bit cache (at most %d)", B, attention_int4_max_groups());
+    return LASER_ERR_CAPACITY;
+  }
   cudaStream_t stream = as_stream(stream_);
   const int K = p->K, Rs = K + 1, n_max = pool ? p->n_max : 1;
   int max_prompt = 0, n_chunks = 0;
@@ -295,7 +299,7 @@ LASER_API laser_status laser_generate(laser_model* m, laser_kv* kv, const laser_
     memset(text + len, 0, size_t(max_total - len) * 4);
     for (int p0 = 0; p0 < len - 1; p0 += kPrefillChunk) chunks.push_back(Chunk{b, p0, std::min(kPrefillChunk, len - 1 - p0)});
   }
-  const std::vector<int> passes = prefill_passes(m, n_chunks);
+  const std::vector<int> passes = prefill_passes(m, kv, n_chunks);
   for (int c0 = 0, i = 0; c0 < n_chunks; c0 += passes[size_t(i++)]) order_pass(chunks.data() + c0, passes[size_t(i)]);
   for (int c = 0; c < n_chunks; ++c) {
     const Chunk& x = chunks[size_t(c)];

@@ -618,8 +618,9 @@ namespace laser {
 // grows with the keys that its rows see, whatever pass they are in, and is left out but for its start.  Against passes as large as they can be,
 // timed in turn, prompts of 256 tokens: 13B (3 layers) 90 chunks 3455 -> 3115 us, 73 2718 -> 2622, 250 8913 -> 9122; 7B (4 layers) 320 chunks
 // 11071 -> 10609, 120 4098 -> 4091, 250 8507 -> 8642, precise 90 5701 -> 5520, 76 4814 -> 4876.  Passes of equal size: 7B 320 chunks 11727, 120 4327.
-std::vector<int> prefill_passes(laser_model* m, int n_chunks) {
-  const int most = std::min(n_chunks, m->R_cap / kPrefillChunk), d = m->cfg.d_model, f = m->cfg.d_ffn;
+std::vector<int> prefill_passes(laser_model* m, const laser_kv* kv, int n_chunks) {
+  const int room = kv->pages4 ? std::min(m->R_cap / kPrefillChunk, attention_int4_max_groups()) : m->R_cap / kPrefillChunk;
+  const int most = std::min(n_chunks, room), d = m->cfg.d_model, f = m->cfg.d_ffn;
   for (int c = int(m->prefill_us.size()); c <= most; ++c) {
     const int rows = c * kPrefillChunk;
     constexpr double kEnds = 4 * 2.5 + 15;   // between launches, and what of the attention does not grow with the rows

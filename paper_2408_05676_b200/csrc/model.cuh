@@ -69,8 +69,9 @@ constexpr int kPrefillShare = 4;    // consecutive chunks that share each staged
 
 void gen_host_free(laser_model* m);
 
-// Chunks of each pass of a prefill of n_chunks, in order: the division whose estimated time is least.
-std::vector<int> prefill_passes(laser_model* m, int n_chunks);
+// Chunks of each pass of a prefill of n_chunks, in order: the division whose estimated time is least, of passes that the workspace and the
+// cache's attention take.
+std::vector<int> prefill_passes(laser_model* m, const laser_kv* kv, int n_chunks);
 
 // The entry points of the same names; `stamp` (optional): the device clock at the end of the rows' making, at the start of the verdict.
 laser_status make_rows(const int32_t* last_token, const int32_t* draft, const int32_t* draft_len, int32_t B, int32_t K, int32_t* tokens,
