@@ -237,7 +237,8 @@ laser_status laser_kv_free(laser_kv* kv);
  * Per token, head and group of 32 features there are codes 0 .. 15, a scale s and a zero z in bf16:
  *   s = bf16((max - min) * (1 / 15)), 0 where that is below 2^-100;  z = bf16(min - 16 s)
  *   code = rint((x - z) / s) - 16, clamped to 0 .. 15 (0 where s = 0), stands for bf16(s (16 + code) + z)
- * each operation in fp32, the quotient (x - z) / s rounded as a division's.
+ * s, z and the code with each operation in fp32, the quotient (x - z) / s rounded as a division's; what the code stands for
+ * rounded once.
  * (NaN is stored as 0 and magnitudes above 2^124 as 2^124: the cache holds finite numbers alone).
  * Every call that takes a cache takes either form: laser_verify_step, _tree, laser_verify_accept and
  * laser_generate write and read it, laser_kv_import rounds to it, laser_kv_export gives the bf16

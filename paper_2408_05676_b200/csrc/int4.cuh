@@ -86,8 +86,14 @@ __device__ __forceinline__ void q4_codes(const float (&x)[4], const Q4Scale& q, 
 }
 // two codes c, d given as 16 + c, 16 + d: c | d << 4 in the low byte, nothing in the next
 __device__ __forceinline__ uint32_t q4_two(float c, float d) { return __float_as_uint(__fmaf_rn(16.f, d, c + (8388608.f - 272.f))); }
-// (the product is exact: eight and five bits)
-__device__ __forceinline__ float q4_held(float at, const Q4Scale& q) { return __fmaf_rn(bf16_value(q.s), at, bf16_value(q.z)); }
+// What two codes c, d stand for, given as 16 + c, 16 + d: the bf16 numbers that the attention kernel makes of them, by the same instruction
+// (rounded once: in fp32 first, a z far below s is lost where s (16 + c) is halfway between two bf16 numbers).
+__device__ __forceinline__ uint32_t q4_held2(float c, float d, const Q4Scale& q) {
+  const __nv_bfloat162 at = __floats2bfloat162_rn(c, d);                   // (whole numbers below 32)
+  uint32_t v;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v) : "r"(*reinterpret_cast<const uint32_t*>(&at)), "r"(q.s | q.s << 16), "r"(q.z | q.z << 16));
+  return v;
+}
 #endif
 
 }  // namespace laser

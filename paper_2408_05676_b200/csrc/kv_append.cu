@@ -204,7 +204,7 @@ kv_append_kernel(const AppendArgs a) {
               *reinterpret_cast<uint16_t*>(p + 4) = uint16_t(sc.z);
             }
           }
-          if (to) held = make_uint2(two_bf16(q4_held(at[0], sc), q4_held(at[1], sc)), two_bf16(q4_held(at[2], sc), q4_held(at[3], sc)));
+          if (to) held = make_uint2(q4_held2(at[0], at[1], sc), q4_held2(at[2], at[3], sc));
         }
         if (to && live) *reinterpret_cast<uint2*>(to + (size_t(r) * count + h) * DH + 4 * l) = held;
       }
@@ -239,9 +239,9 @@ __global__ void export_q4_kernel(const uint8_t* __restrict__ pages, const int32_
       w = __funnelshift_r(w, w, 3 + 8 * (c4 & 1));           // features at bits 0, 16, 4, 20
       codes = (w & 15u) | (w >> 16 & 15u) << 4 | (w >> 4 & 15u) << 8 | (w >> 20 & 15u) << 12;
     }
-    float held[4];
-    for (int u = 0; u < 4; ++u) held[u] = q4_held(float(16 + int(codes >> (4 * u) & 15u)), sc);
-    *reinterpret_cast<uint2*>((is_v ? v : k) + (tok * Hkv + h) * dh + 4 * c4) = make_uint2(two_bf16(held[0], held[1]), two_bf16(held[2], held[3]));
+    float at[4];
+    for (int u = 0; u < 4; ++u) at[u] = float(16 + int(codes >> (4 * u) & 15u));
+    *reinterpret_cast<uint2*>((is_v ? v : k) + (tok * Hkv + h) * dh + 4 * c4) = make_uint2(q4_held2(at[0], at[1], sc), q4_held2(at[2], at[3], sc));
   }
 }
 

@@ -22,6 +22,35 @@ def L():
     return binding
 
 
+def test_values_are_rounded_once(L):
+    """Where s (16 + c) is halfway between two bf16 numbers and the zero, far smaller, decides: what the call hands back, what an export
+    gives and what attention reads are one number, the oracle's."""
+    dim, rng = 128, np.random.default_rng(3)
+    rows = []
+    for e in range(-20, 21):
+        for sign in (1, -1):
+            x = np.full(dim, 32.625, np.float64)
+            x += 1.125 * rng.integers(-11, 2, dim)
+            x[::32], x[1::32] = 18 + sign * 2.0 ** -19, 34.875
+            rows.append(x * 2.0 ** e)
+    x = np.array(rows, np.float32)
+    n = len(rows)
+    want = Q.held(x)
+    _, s, z = Q.quantise(x)
+    assert ((np.abs(z) < s * 2.0 ** -15) & (z != 0)).any()
+    kv = make(L, 1, 1, dim, n, 1)
+    t = torch.as_tensor(x, device="cuda").view(n, 1, dim)
+    ko, vo = (torch.empty(n, 1, 1, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ids, one = dev_i32(range(n)), dev_i32([1] * n)
+    L.kv_append(kv, 0, ids, one, t, t, k_out=ko, v_out=vo)
+    L.kv_check(kv)
+    assert (f64(vo)[:, 0, 0] == want).all() and (f64(ko)[:, 0, 0] == want).all()      # (position 0: no rotation)
+    for i in range(n):
+        assert all((a[0, 0] == want[i]).all() for a in held_rows(L, kv, i, 0, 1)), i
+    q = torch.zeros(n, 1, 1, dim, dtype=torch.bfloat16, device="cuda")
+    assert (f64(L.attend_int4(kv, 0, ids, one, q))[:, 0, 0] == want).all()            # (one token: its value)
+
+
 def test_prompts_of_more_chunks_than_a_launch_takes(L):
     """A workspace that would take all chunks of the prompts in one pass; the text and the cache are those of a small workspace."""
     cfg = synth.model_cfg("tiny", n_layers=2, max_draft=63)
