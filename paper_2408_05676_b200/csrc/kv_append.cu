@@ -217,7 +217,7 @@ kv_append_kernel(const AppendArgs a) {
 
 // What a 4-bit cache holds of tokens [pos0, pos0 + n) of one sequence, as bf16: a thread takes four features of K or V.
 __global__ void export_q4_kernel(const uint8_t* __restrict__ pages, const int32_t* __restrict__ pt, int Hkv, int dh, int pos0, int n,
-                                 bf16* __restrict__ k, bf16* __restrict__ v) {
+                                 int vec, bf16* __restrict__ k, bf16* __restrict__ v) {
   const int c4s = dh / 4;
   const size_t total = size_t(n) * 2 * Hkv * c4s;
   for (size_t idx = size_t(blockIdx.x) * blockDim.x + threadIdx.x; idx < total; idx += size_t(gridDim.x) * blockDim.x) {
@@ -241,7 +241,10 @@ __global__ void export_q4_kernel(const uint8_t* __restrict__ pages, const int32_
     }
     float at[4];
     for (int u = 0; u < 4; ++u) at[u] = float(16 + int(codes >> (4 * u) & 15u));
-    *reinterpret_cast<uint2*>((is_v ? v : k) + (tok * Hkv + h) * dh + 4 * c4) = make_uint2(q4_held2(at[0], at[1], sc), q4_held2(at[2], at[3], sc));
+    const uint2 held = make_uint2(q4_held2(at[0], at[1], sc), q4_held2(at[2], at[3], sc));
+    bf16* to = (is_v ? v : k) + (tok * Hkv + h) * dh + 4 * c4;
+    if (vec) *reinterpret_cast<uint2*>(to) = held;
+    else for (int u = 0; u < 4; ++u) to[u] = reinterpret_cast<const bf16*>(&held)[u];
   }
 }
 
@@ -337,11 +340,11 @@ laser_status kv_copy_q4(const laser_kv* kv, int seq, int layer, int pos0, int n,
     a.vec = four_at_once(k, 0, 2) && four_at_once(v, 0, 2);
     return launch_append(a, n, kv->head_dim, LASER_DTYPE_BF16, stream);
   }
-  LASER_REQUIRE(((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 7) == 0, "k and v must be 8-byte aligned");
+  const int vec = four_at_once(k, 0, 2) && four_at_once(v, 0, 2);
   const size_t total = size_t(n) * 2 * kv->n_kv_heads * (kv->head_dim / 4);
   export_q4_kernel<<<unsigned(std::min<size_t>(ceil_div<size_t>(total, 256), 4096)), 256, 0, stream>>>(
       kv->pages4 + size_t(layer) * kv->layer_bytes4(), kv->page_table + size_t(seq) * kv->pages_per_seq, kv->n_kv_heads, kv->head_dim, pos0, n,
-      static_cast<bf16*>(k), static_cast<bf16*>(v));
+      vec, static_cast<bf16*>(k), static_cast<bf16*>(v));
   count_launch();
   LASER_CUDA(cudaGetLastError());
   return LASER_OK;

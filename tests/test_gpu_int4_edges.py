@@ -79,3 +79,25 @@ def test_generation_of_more_sequences_than_a_step_takes_is_refused_at_once(L):
         L.generate(m, kv, None, [np.array([1], np.int32)] * 1025, [0] * 1025, L.make_params(K=1, max_new=2))
     assert e.value.status == -4
     assert list(L.kv_get_len(kv, range(1025))) == [5] * 1025
+
+
+@pytest.mark.parametrize("int4", [False, True])
+@pytest.mark.parametrize("ko,vo", [(1, 0), (0, 2), (3, 1)])
+def test_copies_to_arrays_that_lie_anywhere(L, int4, ko, vo):
+    """laser_kv_import and _export take arrays of any alignment that their type allows, on either form of the cache."""
+    kv = make(L, 2, 2, 64, 1, 4, int4=int4)
+    rng = np.random.default_rng(4)
+    x = [bf(rng.standard_normal((40, 128))) for _ in range(2)]
+    flat = [torch.zeros(40 * 128 + 8, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    at = [t[o:o + 40 * 128].view(40, 128) for t, o in zip(flat, (ko, vo, ko, vo))]
+    L.kv_import(kv, 0, 0, 3, *x)
+    want = L.kv_export(kv, 0, 0, 3, 40)
+    for t, y in zip(at, x):
+        t.copy_(y)
+    L.kv_import(kv, 0, 0, 20, *at[:2])
+    st = L.lib.laser_kv_export(kv.handle, 0, 0, 20, 40, C.c_void_p(at[2].data_ptr()), C.c_void_p(at[3].data_ptr()), C.c_void_p(0))
+    assert st == 0, L.lib.laser_last_error()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(at[2:], want))
+    for t, o in zip(flat[2:], (ko, vo)):
+        assert (t[:o] == 0).all() and (t[o + 40 * 128:] == 0).all()
