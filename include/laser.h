@@ -348,7 +348,8 @@ laser_status laser_check(laser_model* m, void* stream);
 /* Measurement aid for the forward of Eq. 3: while enabled, every dense-contraction launch
  * (class 0) and every attention launch (class 1) of laser_verify_step is bracketed by CUDA
  * events on the call's stream.  laser_profile_read synchronises the device and returns the
- * summed device time and the number of launches of one class since the previous read. */
+ * summed device time and the number of launches of one class since the previous read.  Over a
+ * 4-bit cache the storing of a layer's rows is a launch of its own, of class 1. */
 laser_status laser_profile_enable(laser_model* m, int32_t on);
 laser_status laser_profile_read(laser_model* m, int32_t cls, double* ms, int64_t* launches);
 

@@ -484,7 +484,7 @@ def profile_enable(model: Model, on: bool) -> None:
 
 
 def profile_read(model: Model, cls: int):
-    """Returns (device ms, launches) of class 0 (dense contractions) or 1 (attention)."""
+    """Returns (device ms, launches) of class 0 (dense contractions) or 1 (attention, storing rows in a 4-bit cache)."""
     ms, n = C.c_double(), C.c_int64()
     _chk(lib.laser_profile_read(model.handle, C.c_int32(cls), C.byref(ms), C.byref(n)))
     return ms.value, n.value

@@ -720,6 +720,7 @@ static laser_status verify_impl(laser_model* m, laser_kv* kv, const int32_t* seq
         ProfScope ps(m, 0, stream);
         LASER_TRY(gemm_fused(m, m->xn, m->wqkv[l] + (kv_alone ? size_t(m->dq) * d : 0), Rp, width, d, EPI_PLAIN, e, stream));
       }
+      ProfScope ps(m, 1, stream);
       LASER_TRY(append_step_rows(m, kv, l, m->qkv, width, !kv_alone, R, stream));
     } else {  // the same; rotary embedding, Q store and cache write in the epilogue
       GemmEpilogue e = base;

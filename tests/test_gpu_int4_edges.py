@@ -101,3 +101,20 @@ def test_copies_to_arrays_that_lie_anywhere(L, int4, ko, vo):
     assert all(torch.equal(a, b) for a, b in zip(at[2:], want))
     for t, o in zip(flat[2:], (ko, vo)):
         assert (t[:o] == 0).all() and (t[o + 40 * 128:] == 0).all()
+
+
+def test_the_profile_counts_every_launch_around_the_cache(L):
+    """Class 1 of laser_profile_read: a layer's attention, and on a 4-bit cache the storing of the step's rows, which is a launch of its
+    own there."""
+    cfg = synth.model_cfg("tiny", n_layers=3)
+    m = L.model_create(cfg, weights_to(synth.make_weights(cfg, seed=0), "cuda"), max_batch=2)
+    ids, n = dev_i32([0, 1]), dev_i32([9, 9])
+    tokens = dev_i32(np.zeros((2, 9)))
+    for create, launches in ((L.kv_create, 3), (L.kv_create_int4, 6)):
+        kv = create(m, 2, 4)
+        L.profile_enable(m, True)
+        L.profile_read(m, 0), L.profile_read(m, 1)
+        L.verify_step(m, kv, ids, tokens, n)
+        gemms, other = L.profile_read(m, 0), L.profile_read(m, 1)
+        L.profile_enable(m, False)
+        assert gemms[1] == 3 * 4 + 1 and other[1] == launches and gemms[0] > 0 and other[0] > 0
