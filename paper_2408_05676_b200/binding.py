@@ -151,6 +151,16 @@ def launch_count() -> int:
     return int(lib.laser_launch_count())
 
 
+def _new(stream, *shape, dtype, device, zero=False) -> torch.Tensor:
+    """Memory for a result of a call on `stream`.  It comes from that stream's own: what the current stream has given back, its work may
+    still use."""
+    make = torch.zeros if zero else torch.empty
+    if stream is None or torch.device(device).type != "cuda":
+        return make(*shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_at(stream), device)):
+        return make(*shape, dtype=dtype, device=device)
+
+
 # ---- pool ------------------------------------------------------------------------------
 class Pool:
     def __init__(self, handle):
@@ -193,9 +203,9 @@ def draft(pool: Pool, tails, tail_len, group_id, params: Params, draft_out=None,
     B = tail_len.shape[0]
     dev = tails.device
     if draft_out is None:
-        draft_out = torch.empty(B, params.K, dtype=torch.int32, device=dev)
-        draft_len = torch.empty(B, dtype=torch.int32, device=dev)
-        match_n = torch.empty(B, dtype=torch.int32, device=dev)
+        draft_out = _new(stream, B, params.K, dtype=torch.int32, device=dev)
+        draft_len = _new(stream, B, dtype=torch.int32, device=dev)
+        match_n = _new(stream, B, dtype=torch.int32, device=dev)
     _chk(lib.laser_draft(pool.handle, _at(tails, torch.int32), _at(tail_len, torch.int32),
                          _at(group_id, torch.int32), B, C.byref(params),
                          _at(draft_out), _at(draft_len), _at(match_n), _stream_at(stream)))
@@ -208,9 +218,9 @@ def draft_temp(pool: Pool, tails, tail_len, group_id, hist, hist_len, params: Pa
     B = tail_len.shape[0]
     dev = tails.device
     if draft_out is None:
-        draft_out = torch.empty(B, params.K, dtype=torch.int32, device=dev)
-        draft_len = torch.empty(B, dtype=torch.int32, device=dev)
-        match_n = torch.empty(B, dtype=torch.int32, device=dev)
+        draft_out = _new(stream, B, params.K, dtype=torch.int32, device=dev)
+        draft_len = _new(stream, B, dtype=torch.int32, device=dev)
+        match_n = _new(stream, B, dtype=torch.int32, device=dev)
     hist = _dev(hist, torch.int32)
     _chk(lib.laser_draft_temp(pool.handle, _ptr(_dev(tails, torch.int32)), _ptr(_dev(tail_len, torch.int32)),
                               _ptr(_dev(group_id, torch.int32)), _ptr(hist), _ptr(_dev(hist_len, torch.int32)),
@@ -223,10 +233,10 @@ def draft_tree(pool: Pool, tails, tail_len, group_id, params: Params, hist=None,
     """laser_draft_tree; returns draft, draft_parents, draft_len, match_n (device tensors)."""
     B = tail_len.shape[0]
     dev = tails.device
-    draft_out = torch.empty(B, params.K, dtype=torch.int32, device=dev)
-    par_out = torch.empty(B, params.K, dtype=torch.int32, device=dev)
-    draft_len = torch.empty(B, dtype=torch.int32, device=dev)
-    match_n = torch.empty(B, dtype=torch.int32, device=dev)
+    draft_out = _new(stream, B, params.K, dtype=torch.int32, device=dev)
+    par_out = _new(stream, B, params.K, dtype=torch.int32, device=dev)
+    draft_len = _new(stream, B, dtype=torch.int32, device=dev)
+    match_n = _new(stream, B, dtype=torch.int32, device=dev)
     stride = 0
     if hist is not None:
         hist, hist_len = _dev(hist, torch.int32), _dev(hist_len, torch.int32)
@@ -241,9 +251,9 @@ def draft_tree(pool: Pool, tails, tail_len, group_id, params: Params, hist=None,
 def make_rows_tree(last_token, draft_t, draft_parents, draft_len, K: int, stream=None):
     B = last_token.shape[0]
     dev = last_token.device
-    tokens = torch.empty(B, K + 1, dtype=torch.int32, device=dev)
-    parents = torch.empty(B, K + 1, dtype=torch.int32, device=dev)
-    n_rows = torch.empty(B, dtype=torch.int32, device=dev)
+    tokens = _new(stream, B, K + 1, dtype=torch.int32, device=dev)
+    parents = _new(stream, B, K + 1, dtype=torch.int32, device=dev)
+    n_rows = _new(stream, B, dtype=torch.int32, device=dev)
     _chk(lib.laser_make_rows_tree(_at(last_token, torch.int32), _at(draft_t, torch.int32),
                                   _at(draft_parents, torch.int32), _at(draft_len, torch.int32),
                                   B, K, _at(tokens), _at(parents), _at(n_rows), _stream_at(stream)))
@@ -253,8 +263,8 @@ def make_rows_tree(last_token, draft_t, draft_parents, draft_len, K: int, stream
 def make_rows(last_token, draft_t, draft_len, K: int, tokens=None, n_rows=None, stream=None):
     B = last_token.shape[0]
     if tokens is None:
-        tokens = torch.empty(B, K + 1, dtype=torch.int32, device=last_token.device)
-        n_rows = torch.empty(B, dtype=torch.int32, device=last_token.device)
+        tokens = _new(stream, B, K + 1, dtype=torch.int32, device=last_token.device)
+        n_rows = _new(stream, B, dtype=torch.int32, device=last_token.device)
     _chk(lib.laser_make_rows(_at(last_token, torch.int32), _at(draft_t, torch.int32),
                              _at(draft_len, torch.int32), B, K,
                              _at(tokens), _at(n_rows), _stream_at(stream)))
@@ -375,7 +385,7 @@ def kv_append(kv: KV, layer: int, seq_ids, n_rows, k, v, q=None, parents=None, q
     if q is not None:
         qa, qs = _rows_at(q, dtype, B, rows, H * dh, dev)
         if q_out is None:
-            q_out = torch.empty(B, rows, H, dh, dtype=_BF16, device=k.device)
+            q_out = _new(stream, B, rows, H, dh, dtype=_BF16, device=k.device)
     if q_out is not None:
         qo = _adr(q_out, _BF16, (B, rows, H, dh), dev)
     held = (B, rows, Hkv, dh)
@@ -396,7 +406,7 @@ def attend_int4(kv: KV, layer: int, seq_ids, n_rows, q, parents=None, out=None, 
     B, rows = n[0], n[1]
     dev, st = _home(q, stream)
     if out is None:
-        out = torch.empty(B, rows, cfg["n_heads"], cfg["head_dim"], dtype=_BF16, device=q.device)
+        out = _new(stream, B, rows, cfg["n_heads"], cfg["head_dim"], dtype=_BF16, device=q.device)
     qa, qs = _rows_at(q, _BF16, B, rows, width, dev)
     oa, os_ = _rows_at(out, _BF16, B, rows, width, dev)
     status = lib.laser_attend_int4(kv.handle, layer, _adr(seq_ids, _I32, (B,), dev), None if parents is None else _adr(parents, _I32, (B, rows), dev),
@@ -446,8 +456,8 @@ def kv_import(kv: KV, seq: int, layer: int, pos0: int, k: torch.Tensor, v: torch
 def kv_export(kv: KV, seq: int, layer: int, pos0: int, n: int, stream=None):
     cfg = kv.model.cfg
     w = cfg["n_kv_heads"] * cfg["head_dim"]
-    k = torch.empty(n, w, dtype=torch.bfloat16, device="cuda")
-    v = torch.empty(n, w, dtype=torch.bfloat16, device="cuda")
+    k = _new(stream, n, w, dtype=torch.bfloat16, device="cuda")
+    v = _new(stream, n, w, dtype=torch.bfloat16, device="cuda")
     _chk(lib.laser_kv_export(kv.handle, C.c_int32(seq), C.c_int32(layer), C.c_int32(pos0), C.c_int32(n),
                              _ptr(k), _ptr(v), _stream(stream)))
     return k, v
@@ -458,7 +468,7 @@ def verify_step(model: Model, kv: KV, seq_ids, tokens, n_rows, logits=None, stre
     R = model.cfg["max_draft"] + 1
     assert tokens.shape == (B, R), (tokens.shape, B, R)
     if logits is None:
-        logits = torch.empty(B, R, model.cfg["vocab"], dtype=torch.float32, device=tokens.device)
+        logits = _new(stream, B, R, model.cfg["vocab"], dtype=torch.float32, device=tokens.device)
     _chk(lib.laser_verify_step(model.handle, kv.handle, _ptr(_dev(seq_ids, torch.int32)),
                                _ptr(_dev(tokens, torch.int32)), _ptr(_dev(n_rows, torch.int32)),
                                C.c_int32(B), _ptr(_dev(logits, torch.float32)), _stream(stream)))
@@ -471,7 +481,7 @@ def verify_step_tree(model: Model, kv: KV, seq_ids, tokens, parents, n_rows, log
     R = model.cfg["max_draft"] + 1
     assert tokens.shape == (B, R) and parents.shape == (B, R), (tokens.shape, parents.shape, B, R)
     if logits is None:
-        logits = torch.empty(B, R, model.cfg["vocab"], dtype=torch.float32, device=tokens.device)
+        logits = _new(stream, B, R, model.cfg["vocab"], dtype=torch.float32, device=tokens.device)
     _chk(lib.laser_verify_step_tree(model.handle, kv.handle, _ptr(_dev(seq_ids, torch.int32)),
                                     _ptr(_dev(tokens, torch.int32)), _ptr(_dev(parents, torch.int32)),
                                     _ptr(_dev(n_rows, torch.int32)), C.c_int32(B), _ptr(_dev(logits, torch.float32)),
@@ -495,7 +505,7 @@ def check(model: Model, stream=None) -> None:
 
 
 def selftest_wait(model: Model, limit_cycles: int, stream=None) -> torch.Tensor:
-    report = torch.zeros(4, dtype=torch.int32, device="cuda")
+    report = _new(stream, 4, dtype=torch.int32, device="cuda", zero=True)
     _chk(lib.laser_selftest_wait(model.handle, C.c_int64(int(limit_cycles)), _ptr(report), _stream(stream)))
     return report
 
@@ -514,7 +524,7 @@ def adjust_logits(logits, tokens, n_rows, hist=None, hist_len=None, prompt_len=N
     B, R, V = shape = logits.shape
     dev, st = _home(logits, stream)
     if out is None:
-        out = torch.empty_like(logits)
+        out = _new(stream, *shape, dtype=_F32, device=logits.device)
     one, rows = (B,), (B, R)
     ha = hl = stride = pl = rep = freq = pres = off = ids = val = words = ss = rs = None
     if hist is not None:
@@ -564,8 +574,8 @@ def accept_commit(kv: Optional[KV], seq_ids, logits, tokens, n_rows, params: Par
     assert R == params.K + 1 and tokens.shape == (B, R)
     if out is None:
         dev = logits.device
-        out = (torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B, R, dtype=torch.int32, device=dev),
-               torch.empty(B, dtype=torch.int32, device=dev))
+        out = (_new(stream, B, dtype=torch.int32, device=dev), _new(stream, B, R, dtype=torch.int32, device=dev),
+               _new(stream, B, dtype=torch.int32, device=dev))
     n_accept, out_tokens, n_out = out
     _chk(lib.laser_accept_commit(kv.handle if kv is not None else None,
                                  _at(seq_ids),
@@ -584,8 +594,8 @@ def verify_accept(model: Model, kv: KV, seq_ids, tokens, n_rows, params: Params,
     assert tokens.shape == (B, R), (tokens.shape, B, R)
     if out is None:
         dev = tokens.device
-        out = (torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B, R, dtype=torch.int32, device=dev),
-               torch.empty(B, dtype=torch.int32, device=dev))
+        out = (_new(stream, B, dtype=torch.int32, device=dev), _new(stream, B, R, dtype=torch.int32, device=dev),
+               _new(stream, B, dtype=torch.int32, device=dev))
     n_accept, out_tokens, n_out = out
     _chk(lib.laser_verify_accept(model.handle, kv.handle, _ptr(_dev(seq_ids, torch.int32)), _ptr(_dev(tokens, torch.int32)),
                                  _ptr(_dev(n_rows, torch.int32)), C.c_int32(B), C.byref(params), C.c_int32(1 if commit else 0),
@@ -598,10 +608,10 @@ def accept_tree(kv: Optional[KV], seq_ids, logits, tokens, parents, n_rows, para
     """laser_accept_tree; returns n_accept, out_tokens, n_out, path_rows (device tensors)."""
     B, R, V = logits.shape
     dev = logits.device
-    n_accept = torch.empty(B, dtype=torch.int32, device=dev)
-    out_tokens = torch.empty(B, R, dtype=torch.int32, device=dev)
-    n_out = torch.empty(B, dtype=torch.int32, device=dev)
-    path_rows = torch.empty(B, R, dtype=torch.int32, device=dev)
+    n_accept = _new(stream, B, dtype=torch.int32, device=dev)
+    out_tokens = _new(stream, B, R, dtype=torch.int32, device=dev)
+    n_out = _new(stream, B, dtype=torch.int32, device=dev)
+    path_rows = _new(stream, B, R, dtype=torch.int32, device=dev)
     _chk(lib.laser_accept_tree(kv.handle if kv is not None else C.c_void_p(0),
                                _ptr(_dev(seq_ids, torch.int32)) if seq_ids is not None else C.c_void_p(0),
                                _ptr(_dev(logits, torch.float32)), _ptr(_dev(tokens, torch.int32)),
@@ -626,8 +636,8 @@ def group_kmeans(x: torch.Tensor, centroids: torch.Tensor, iters: int, stream=No
     assert centroids.is_cuda and centroids.dtype == torch.float32 and centroids.is_contiguous()
     n, dim = x.shape
     k = centroids.shape[0]
-    assign = torch.empty(n, dtype=torch.int32, device=x.device)
-    counts = torch.empty(k, dtype=torch.int32, device=x.device)
+    assign = _new(stream, n, dtype=torch.int32, device=x.device)
+    counts = _new(stream, k, dtype=torch.int32, device=x.device)
     _chk(lib.laser_group_kmeans(_ptr(x), C.c_int64(n), C.c_int32(dim), C.c_int32(k), C.c_int32(iters),
                                 _ptr(centroids), _ptr(assign), _ptr(counts), _stream(stream)))
     return assign, counts

@@ -76,3 +76,62 @@ def test_a_model_that_first_meets_a_4bit_cache_in_a_step(L):
         torch.cuda.synchronize()
         L.check(other)
         assert all(torch.equal(x, want) for x in logits)
+
+
+def _calls_with_results(L):
+    """Calls whose result the binding allocates: a call on a stream, by name."""
+    cfg = synth.model_cfg("tiny", n_layers=1, d_model=64, d_ffn=64, vocab=64, n_heads=4, n_kv_heads=4, head_dim=64, max_draft=3)
+    m = L.model_create(cfg, weights_to(synth.make_weights(cfg, seed=0), "cuda"), max_batch=4)
+    caches = [L.kv_create(m, 4, 16), L.kv_create_int4(m, 4, 16)]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn(4, 4, 256, device="cuda", generator=g).to(torch.bfloat16)
+    ids, n = dev_i32(range(4)), dev_i32([4] * 4)
+    for kv in caches:
+        L.kv_append(kv, 0, ids, n, x, x)
+    tokens = dev_i32(np.arange(16).reshape(4, 4))
+    chain = dev_i32([[-1, 0, 1, 2]] * 4)
+    logits = torch.randn(4, 4, 64, device="cuda", generator=g)
+    docs = [[list(range(60)) * 3] for _ in range(4)]
+    pool_tokens, offs = synth.pool_from_documents(docs)
+    pool = L.pool_build(pool_tokens, offs, 1, 3)
+    prm = L.make_params(K=3, n_min=1, n_max=3, max_occ=64)
+    tails, tail_len = dev_i32([[3, 4, 5]] * 4), dev_i32([3] * 4)
+    hist, hist_len = dev_i32(np.tile(np.arange(20), (4, 1))), dev_i32([20] * 4)
+    draft, draft_len = dev_i32([[6, 7, 8]] * 4), dev_i32([3] * 4)
+    last = dev_i32([5] * 4)
+    return dict(
+        draft=lambda s: L.draft(pool, tails, tail_len, ids, prm, stream=s),
+        draft_temp=lambda s: L.draft_temp(pool, tails, tail_len, ids, hist, hist_len, prm, stream=s),
+        draft_tree=lambda s: L.draft_tree(pool, tails, tail_len, ids, prm, stream=s),
+        make_rows=lambda s: L.make_rows(last, draft, draft_len, 3, stream=s),
+        make_rows_tree=lambda s: L.make_rows_tree(last, draft, dev_i32([[0, 1, 2]] * 4), draft_len, 3, stream=s),
+        kv_append=lambda s: L.kv_append(caches[1], 0, ids, n, x, x, q=x, stream=s),
+        attend_int4=lambda s: L.attend_int4(caches[1], 0, ids, n, x, stream=s),
+        kv_export=lambda s: L.kv_export(caches[0], 1, 0, 0, 4, stream=s),
+        verify_step=lambda s: L.verify_step(m, caches[1], ids, tokens, n, stream=s),
+        verify_step_tree=lambda s: L.verify_step_tree(m, caches[0], ids, tokens, chain, n, stream=s),
+        adjust_logits=lambda s: L.adjust_logits(logits, tokens, n, stream=s),
+        accept_commit=lambda s: L.accept_commit(None, None, logits, tokens, n, prm, stream=s),
+        accept_tree=lambda s: L.accept_tree(None, None, logits, tokens, chain, n, prm, stream=s),
+        verify_accept=lambda s: L.verify_accept(m, caches[1], ids, tokens, n, prm, commit=False, stream=s),
+    )
+
+
+def test_results_belong_to_the_stream_of_the_call(L):
+    """The current stream still has work to do on memory that was given back: a call on another stream must not get that memory for
+    its result."""
+    stream = torch.cuda.Stream(priority=-1)
+    flat = lambda r: [t for t in (r if isinstance(r, tuple) else (r,)) if t is not None]
+    for name, call in _calls_with_results(L).items():
+        want = [t.clone() for t in flat(call(None))]
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        stale = [torch.empty_like(t) for t in want]
+        torch.cuda._sleep(40_000_000)                        # (some 20 ms)
+        for t in stale:
+            t.fill_(7)
+        del stale, t
+        got = flat(call(stream if name != "make_rows" else stream.cuda_stream))          # (a handle will do as well)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), name
