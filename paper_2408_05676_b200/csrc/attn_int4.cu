@@ -152,7 +152,9 @@ struct Segment { int b, hk, row0, start, blocks; };
 // one that is cut: the teams whose pieces are this CTA's; whether the last of them went on behind it; whether other CTAs have pieces, and
 // then whether they have its beginning
 struct Cut { Segment seg; int first, last; bool early, open, begun; };
-constexpr float kNothing = 1e30f;      // -m of rows that have seen nothing
+// -m of rows that have seen nothing: above every score x scale that 32 bits hold (6.1e37), so that the first score a row sees, however low,
+// gives it a reference
+constexpr float kNothing = 1e38f;
 
 template <int DH, int NT>
 __global__ void __launch_bounds__(Sizes<DH, NT>::kWarps * 32, 1)
@@ -410,12 +412,15 @@ attn_int4_kernel(const AttnArgs a) {
         // probabilities: from (token, row) to the second product's fragments, a row's tokens 2 qd, 2 qd + 1 (and 8 on) in lane g
         uint32_t p[NT][2];
         uint2* const team_p = reinterpret_cast<uint2*>(region + S * ST * BLK + Z::kQBytes + (it & 1) * Z::kPBytes) + lane;
+        // The reference came of a product rounded to 32 bits, so the products are rounded, too, before it is added: in one step (2 % less for one
+        // row's time over long texts) what that rounding dropped would be left as an exponent, without bound where scores are above 2^24.
+        auto exponent = [&](int t, int c) { return __fadd_rn(__fmul_rn(x[t][c], a.scale), shift[t][c & 1]); };
         auto probabilities = [&]() {        // whether one is above 2^6
           uint32_t highest = 0;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            p[t][0] = pack_bf16(ex2(fmaf(x[t][0], a.scale, shift[t][0])), ex2(fmaf(x[t][1], a.scale, shift[t][1])));
-            p[t][1] = pack_bf16(ex2(fmaf(x[t][2], a.scale, shift[t][0])), ex2(fmaf(x[t][3], a.scale, shift[t][1])));
+            p[t][0] = pack_bf16(ex2(exponent(t, 0)), ex2(exponent(t, 1)));
+            p[t][1] = pack_bf16(ex2(exponent(t, 2)), ex2(exponent(t, 3)));
             highest = max2(highest, max2(p[t][0], p[t][1]));
             p[t][0] = transpose8(p[t][0]);
             p[t][1] = transpose8(p[t][1]);
@@ -443,7 +448,7 @@ attn_int4_kernel(const AttnArgs a) {
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
               if (S == 2) top[t][y] = fmaxf(top[t][y], s_half[S == 1 ? 0 : warp ^ 1][8 * t + 2 * qd + y]);
-              const float next = fminf(shift[t][y], -ceilf(top[t][y] * a.scale));
+              const float next = fminf(shift[t][y], -ceilf(__fmul_rn(top[t][y], a.scale)));
               down[y] = ex2(next - shift[t][y]);
               shift[t][y] = next;
             }

@@ -51,6 +51,38 @@ def test_values_are_rounded_once(L):
     assert (f64(L.attend_int4(kv, 0, ids, one, q))[:, 0, 0] == want).all()            # (one token: its value)
 
 
+@pytest.mark.parametrize("rows", [1, 9, 33])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_scores_of_any_size(L, rows, dim):
+    """All scores far below zero, up to the largest numbers that 32 bits hold; texts whose scores jump there and back.  Equal scores weigh
+    the same, and what is far below a row's highest weighs nothing."""
+    n = 75
+    sizes = [-1e10, -1e22, -1e33, 1e10, 1e33, -3.0e37 / 2 ** 4, "low then normal", "normal then low", "high once"]
+    kv = make(L, 2, 1, dim, len(sizes), 8)
+    rng = np.random.default_rng(2)
+    q = np.zeros((len(sizes), rows, 2, dim), np.float32)
+    q[..., 0], q[..., 1] = 1, -1
+    k, v = np.zeros((len(sizes), n, dim)), rng.standard_normal((len(sizes), n, dim))
+    for s, size in enumerate(sizes):
+        big = np.zeros(n)
+        if isinstance(size, float):
+            big[:] = size
+        elif size == "high once":
+            big[41] = 1e30
+        else:
+            big[(slice(0, 40) if size == "low then normal" else slice(40, n))] = -1e33
+        k[s, :, 0] = big
+        L.kv_import(kv, s, 0, 0, bf(k[s]), bf(v[s]))
+    L.kv_set_len(kv, range(len(sizes)), [n - rows] * len(sizes))
+    out = f64(L.attend_int4(kv, 0, dev_i32(range(len(sizes))), dev_i32([rows] * len(sizes)), torch.as_tensor(q, device="cuda").to(torch.bfloat16)))
+    L.kv_check(kv)
+    for s in range(len(sizes)):
+        held_k, held_v = held_rows(L, kv, s, 0, n)
+        want, spread = Q.attend(q[s].astype(np.float64), held_k, held_v, n - rows, Q.paths(rows))
+        tol = HALF * (1 + 2.0 ** -7) * spread + 2.0 ** -16 * (spread + np.abs(want)) + HALF * np.abs(want) + 2.0 ** -24
+        assert (np.abs(out[s] - want) <= tol).all(), sizes[s]
+
+
 def test_prompts_of_more_chunks_than_a_launch_takes(L):
     """A workspace that would take all chunks of the prompts in one pass; the text and the cache are those of a small workspace."""
     cfg = synth.model_cfg("tiny", n_layers=2, max_draft=63)
