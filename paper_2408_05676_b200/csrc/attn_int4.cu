@@ -156,6 +156,13 @@ struct Cut { Segment seg; int first, last; bool early, open, begun; };
 // gives it a reference
 constexpr float kNothing = 1e38f;
 
+// ceil(total / parts), parts below 2^16; in 32 bits where they hold total + parts (in 64 a division takes 100 instructions)
+__host__ __device__ constexpr int share_of(long long total, unsigned parts) {
+  return total <= 0xffffffffll - 0xffff ? int((unsigned(total) + parts - 1) / parts) : int((total + parts - 1) / parts);
+}
+static_assert(share_of(0xffffffffll, 148) == 29020050 && share_of(0xffffffffll - 0xffff, 148) == 29019607 && share_of(0x100000000ll, 148) == 29020050 &&
+              share_of(149, 148) == 2 && share_of(1, 148) == 1, "");
+
 template <int DH, int NT>
 __global__ void __launch_bounds__(Sizes<DH, NT>::kWarps * 32, 1)
 attn_int4_kernel(const AttnArgs a) {
@@ -234,7 +241,7 @@ attn_int4_kernel(const AttnArgs a) {
   if (a.row_ctx) wait_for_earlier();
   // (below 2^31: launch_attention sees to it)
   constexpr int kLeast = 2 / S;        // blocks of a team: two pages are in flight together anyway
-  const int per_cta = max(total <= 0xffffffffll ? int((unsigned(total) + gridDim.x - 1) / gridDim.x) : int((total + gridDim.x - 1) / gridDim.x), 2 * kLeast);
+  const int per_cta = max(share_of(total, gridDim.x), 2 * kLeast);
   const long long c0 = (long long)per_cta * blockIdx.x;
   if (tid == 0) a.joins[blockIdx.x].count = 0;
   if (c0 >= total) return;
