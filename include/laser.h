@@ -244,6 +244,8 @@ laser_status laser_kv_free(laser_kv* kv);
  * laser_generate write and read it, laser_kv_import rounds to it, laser_kv_export gives the bf16
  * numbers that it stands for, and laser_accept_tree / laser_kv_compact_path move codes as they are.
  * Logits are those of a model whose keys and values are rounded this way; 1024 sequences a step at most.
+ * As over a bf16 cache, a row's bits do not depend on its place in the step, so that strict decoding gives
+ * plain greedy decoding's text.
  * The first such cache of a model also allocates fp32 rows for a layer's projections (a model that did
  * not create the cache does so in its first step over it, which must not be under stream capture).
  * Errors: UNSUPPORTED (head_dim other than 64 and 128, a precise model), INVALID_ARG, OOM. */
@@ -302,10 +304,12 @@ laser_status laser_kv_append(laser_kv* kv, int32_t layer, const int32_t* seq_ids
  *   q    dev bf16 rows of n_heads * head_dim, q_stride elements apart, 16-byte aligned rows
  *   out  dev bf16 rows likewise, out_stride apart, 4-byte aligned; rows that are not active are left
  *        as they are
- * The work is divided evenly over the SMs whatever the lengths.  It keeps partial results in memory of
- * the cache's.  Asynchronous on `stream`.
+ * In calls of one shape (B, rows, the same cache) a row's bits follow from itself and what it sees:
+ * not from its place among the rows, nor from what the other sequences are, how long they are and which
+ * rows of them are active.  It keeps partial results in memory of the cache's.  Asynchronous on `stream`.
  * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 1024, or tiles of up to 40
- * rows x pages beyond 2^31 for a sequence or, of all, for an SM); on the device as above. */
+ * rows x pages beyond 2^31 for a sequence or, of all, for an SM, or more tiles than 2^31); on the device
+ * as above. */
 laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int32_t* seq_ids, const int32_t* parents,
                                const int32_t* n_rows, int32_t B, int32_t rows, const void* q, int64_t q_stride,
                                void* out, int64_t out_stride, void* stream);

@@ -490,8 +490,8 @@ LASER_API laser_status laser_kv_create_int4(laser_model* m, int32_t max_seqs, in
   LASER_CUDA(cudaMemset(kv->pages4, 0, bytes));      // scales and zeros of 0: finite, as masked tokens have to be
   int dev = 0;
   LASER_CUDA(cudaGetDevice(&dev));
-  LASER_CUDA(cudaDeviceGetAttribute(&kv->attn_ctas, cudaDevAttrMultiProcessorCount, dev));
-  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->attn_part), attention_int4_part_floats(kv->head_dim, kv->attn_ctas) * sizeof(float)));
+  LASER_CUDA(cudaDeviceGetAttribute(&kv->attn_sms, cudaDevAttrMultiProcessorCount, dev));
+  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->attn_part), attention_int4_part_floats(kv->head_dim, kv->attn_sms) * sizeof(float)));
   LASER_TRY(memsets_done());
   guard.p = nullptr;
   *out = kv;

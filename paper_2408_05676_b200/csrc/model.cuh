@@ -171,7 +171,7 @@ laser_status append_step_rows(laser_model* m, laser_kv* kv, int layer, const flo
 laser_status attention_int4_launch(laser_model* m, laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* parents, int B, int Rs,
                                    cudaStream_t stream);
 int attention_int4_max_groups();                                  // most sequences or prompt chunks of a launch
-size_t attention_int4_part_floats(int head_dim, int ctas);        // room for its partial results
+size_t attention_int4_part_floats(int head_dim, int sms);        // room for its partial results
 laser_status kv_copy_q4(const laser_kv* kv, int seq, int layer, int pos0, int n, void* k, void* v, bool to_pages, cudaStream_t stream);
 laser_status compact_path_q4(laser_kv* kv, const int32_t* seq_ids, const int32_t* path_rows, const int32_t* n_accept, int B, int row_stride,
                              cudaStream_t stream);

@@ -22,7 +22,7 @@ struct laser_kv {
   int32_t* status = nullptr;      // dev: first device-side error of the calls on the cache itself, 0 = none
   // attention over a 4-bit cache: partial results of a call
   float* attn_part = nullptr;
-  int32_t attn_ctas = 0;
+  int32_t attn_sms = 0;
   size_t page_elems() const { return size_t(2) * n_kv_heads * page_size * head_dim; }
   size_t layer_elems() const { return size_t(n_pages) * page_elems(); }
   size_t layer_bytes4() const { return size_t(n_pages) * n_kv_heads * 20 * head_dim; }
