@@ -246,8 +246,10 @@ laser_status laser_kv_free(laser_kv* kv);
  * Logits are those of a model whose keys and values are rounded this way; 1024 sequences a step at most.
  * As over a bf16 cache, a row's bits do not depend on its place in the step, so that strict decoding gives
  * plain greedy decoding's text.
- * The first such cache of a model also allocates fp32 rows for a layer's projections (a model that did
- * not create the cache does so in its first step over it, which must not be under stream capture).
+ * The first such cache of a model also allocates fp32 rows for a layer's projections and room for
+ * partial results, for all its steps over such caches (a model that did not create one does so in its
+ * first step over one, which must not be under stream capture).  Steps of two models over one cache may
+ * run at the same time, as over a bf16 cache, if their sequences are not the same.
  * Errors: UNSUPPORTED (head_dim other than 64 and 128, a precise model), INVALID_ARG, OOM. */
 laser_status laser_kv_create_int4(laser_model* m, int32_t max_seqs, int64_t n_pages, laser_kv** out);
 /* host int32[max_seqs * pages_per_seq]: physical page of each logical page; every entry
@@ -276,7 +278,8 @@ laser_status laser_kv_export(const laser_kv* kv, int32_t seq, int32_t layer, int
  * their own.  The rows of sequence b are 0 .. n_rows[b]-1 (clamped to 0 .. rows); row i has the
  * position len + i and goes to cache slot len + i.  With parents (dev int32[B, rows], as
  * laser_verify_step_tree; rows <= 64) its position is len + depth(i).  Committed lengths are read
- * and not changed.  seq_ids must be distinct.  Calls on one cache must not overlap on the GPU.
+ * and not changed.  seq_ids must be distinct.  Two calls of laser_attend_int4 on one cache must not
+ * run at the same time, nor others where one's sequences are the other's.
  *
  * laser_kv_append: q and k are rotated (rotate-half pairing, the model's rope_theta, angles in 64
  * bits), k and v go to the cache, of either form.

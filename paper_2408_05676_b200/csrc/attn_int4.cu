@@ -613,14 +613,15 @@ int row_tiles(int rows) {
   return ceil_div(ceil_div(rows, tiles), 8);
 }
 
-laser_status launch_attention(const laser_kv* kv, int n_heads, AttnArgs a, cudaStream_t stream) {
+// `part`: room for partial results, which calls that may run at the same time do not share.
+laser_status launch_attention(const laser_kv* kv, int n_heads, AttnArgs a, float* part, cudaStream_t stream) {
   a.max_seqs = kv->max_seqs;
   a.capacity = int(std::min<int64_t>(kv->capacity_tokens(), INT32_MAX));
   a.Hkv = kv->n_kv_heads; a.G = n_heads / kv->n_kv_heads;
   a.page_table = kv->page_table; a.pages_per_seq = kv->pages_per_seq;
   a.scale = float(1.4426950408889634 / std::sqrt(double(kv->head_dim)));
   a.group_inv = unsigned(((uint64_t(1) << 32) + a.G - 1) / a.G);
-  a.records = kv->attn_part;
+  a.records = part;
   const int64_t rows = int64_t(a.Rs) * a.G;
   const int nt = row_tiles(int(std::min<int64_t>(rows, 1 << 28)));
   const int64_t tiles = ceil_div(rows, int64_t(8 * nt)), units = int64_t(a.B) * a.Hkv * tiles;
@@ -689,7 +690,7 @@ laser_status attention_int4_launch(laser_model* m, laser_kv* kv, int layer, cons
   a.q = m->q; a.out = m->attn;
   a.ldq = a.ldo = m->dq;         // (the model's heads: another of the same cache shape may have made the cache)
   a.status = m->status;
-  return launch_attention(kv, m->cfg.n_heads, a, stream);
+  return launch_attention(kv, m->cfg.n_heads, a, m->attn4_part, stream);
 }
 
 }  // namespace laser
@@ -716,5 +717,5 @@ LASER_API laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int3
   a.q = static_cast<const __nv_bfloat16*>(q); a.out = static_cast<__nv_bfloat16*>(out);
   a.ldq = q_stride; a.ldo = out_stride;
   a.status = kv->status;
-  return launch_attention(kv, kv->n_heads, a, as_stream(stream));
+  return launch_attention(kv, kv->n_heads, a, kv->attn_part, as_stream(stream));
 }

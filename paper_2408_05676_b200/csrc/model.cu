@@ -268,6 +268,13 @@ laser_status memsets_done() {
   return LASER_OK;
 }
 
+laser_status sm_count(int* n) {
+  int dev = 0;
+  LASER_CUDA(cudaGetDevice(&dev));
+  LASER_CUDA(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
+  return LASER_OK;
+}
+
 // Returns `first` if the pieces are adjacent in memory, else a fused device copy.
 laser_status fuse_rows(laser_model* m, const void* const* pieces, const size_t* elems, int n,
                        const bf16** out) {
@@ -288,15 +295,22 @@ laser_status fuse_rows(laser_model* m, const void* const* pieces, const size_t* 
   return LASER_OK;
 }
 
-// Rows for a layer's projections, which a step over a 4-bit cache keeps in fp32 until they are rotated and stored.  Not zeroed: the projection
-// writes every row that is read, and a memset would not be in the order of the step's stream.
-laser_status qkv_rows(laser_model* m) {
-  if (m->qkv) return LASER_OK;
-  float* rows = nullptr;
-  LASER_CUDA(device_malloc(reinterpret_cast<void**>(&rows), size_t(m->R_cap) * m->dqkv * sizeof(float)));
-  m->owned.push_back(rows);
-  m->qkv = rows;
-  return LASER_OK;
+// What a model's steps over 4-bit caches keep: rows for a layer's projections, in fp32 until they are rotated and stored, and attention's partial
+// results.  Not zeroed: what is read was written before, and a memset would not be in the order of the step's stream.
+laser_status int4_workspace(laser_model* m) {
+  auto room = [&](float** p, size_t floats) -> laser_status {
+    if (*p) return LASER_OK;
+    float* rows = nullptr;
+    LASER_CUDA(device_malloc(reinterpret_cast<void**>(&rows), floats * sizeof(float)));
+    m->owned.push_back(rows);
+    *p = rows;
+    return LASER_OK;
+  };
+  LASER_TRY(room(&m->qkv, size_t(m->R_cap) * m->dqkv));
+  if (m->attn4_part) return LASER_OK;
+  int sms = 0;
+  LASER_TRY(sm_count(&sms));
+  return room(&m->attn4_part, attention_int4_part_floats(m->cfg.head_dim, sms));
 }
 
 }  // namespace
@@ -481,16 +495,14 @@ LASER_API laser_status laser_kv_create_int4(laser_model* m, int32_t max_seqs, in
   LASER_REQUIRE(max_seqs >= 1 && n_pages >= max_seqs, "max_seqs = %d, n_pages = %lld", max_seqs, (long long)n_pages);
   if (m->cfg.head_dim != 64 && m->cfg.head_dim != 128) { set_error("head_dim = %d (a 4-bit cache needs 64 or 128)", m->cfg.head_dim); return LASER_ERR_UNSUPPORTED; }
   if (m->precise) { set_error("a precise model keeps its cache in bf16"); return LASER_ERR_UNSUPPORTED; }
-  LASER_TRY(qkv_rows(m));
+  LASER_TRY(int4_workspace(m));
   laser_kv* kv = new laser_kv();
   struct Guard { laser_kv* p; ~Guard() { if (p) laser_kv_free(p); } } guard{kv};
   LASER_TRY(kv_open(m, max_seqs, n_pages, kv));
   const size_t bytes = std::max<size_t>(16, size_t(kv->n_layers) * kv->layer_bytes4());
   LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->pages4), bytes));
   LASER_CUDA(cudaMemset(kv->pages4, 0, bytes));      // scales and zeros of 0: finite, as masked tokens have to be
-  int dev = 0;
-  LASER_CUDA(cudaGetDevice(&dev));
-  LASER_CUDA(cudaDeviceGetAttribute(&kv->attn_sms, cudaDevAttrMultiProcessorCount, dev));
+  LASER_TRY(sm_count(&kv->attn_sms));
   LASER_CUDA(device_malloc(reinterpret_cast<void**>(&kv->attn_part), attention_int4_part_floats(kv->head_dim, kv->attn_sms) * sizeof(float)));
   LASER_TRY(memsets_done());
   guard.p = nullptr;
@@ -674,7 +686,7 @@ static laser_status verify_impl(laser_model* m, laser_kv* kv, const int32_t* seq
   if (q4) {
     if (m->precise) { set_error("a precise model needs a bf16 cache"); return LASER_ERR_UNSUPPORTED; }
     if (B > attention_int4_max_groups()) { set_error("B = %d sequences over a 4-bit cache (at most %d)", B, attention_int4_max_groups()); return LASER_ERR_CAPACITY; }
-    LASER_TRY(qkv_rows(m));
+    LASER_TRY(int4_workspace(m));
   }
   // the LM head stores four logits at a time
   LASER_REQUIRE((reinterpret_cast<uintptr_t>(logits) & 15) == 0, "logits must be 16-byte aligned");

@@ -27,6 +27,7 @@ struct laser_model {
   __nv_bfloat16* act = nullptr;    // [R_cap, f] SwiGLU output
   float* sumsq = nullptr;          // [ceil(d/128)][R_cap] per-tile sums of squares of the residual
   float* qkv = nullptr;            // [R_cap, dqkv] projections of a layer in fp32: steps over a 4-bit cache only, made with the first such cache
+  float* attn4_part = nullptr;     // partial results of attention over a 4-bit cache, made with them
   float* rope = nullptr;           // [R_cap, head_dim/2, 2] cos, sin of each row's position
   int32_t* row_pos = nullptr;      // [R_cap] position of the row, -1 = inactive
   int32_t* row_seq = nullptr;      // [R_cap] cache slot of the row

@@ -20,7 +20,7 @@ struct laser_kv {
   bool has_pages_map = false;
   double* inv_freq = nullptr;     // dev [head_dim / 2] theta^(-2j / head_dim)
   int32_t* status = nullptr;      // dev: first device-side error of the calls on the cache itself, 0 = none
-  // attention over a 4-bit cache: partial results of a call
+  // attention over a 4-bit cache: partial results of laser_attend_int4 (a step's are its model's)
   float* attn_part = nullptr;
   int32_t attn_sms = 0;
   size_t page_elems() const { return size_t(2) * n_kv_heads * page_size * head_dim; }

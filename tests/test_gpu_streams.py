@@ -78,6 +78,33 @@ def test_a_model_that_first_meets_a_4bit_cache_in_a_step(L):
         assert all(torch.equal(x, want) for x in logits)
 
 
+def test_two_models_step_over_one_4bit_cache_at_once(L):
+    """On streams of their own, over sequences of their own: neither sees the other's partial results."""
+    cfg = synth.model_cfg("tiny", n_layers=4, d_model=512, n_heads=8, n_kv_heads=2, head_dim=64, max_draft=8)
+    models = [L.model_create(cfg, weights_to(synth.make_weights(cfg, seed=s), "cuda"), max_batch=2) for s in (1, 2)]
+    kv = L.kv_create_int4(models[0], 4, 4 * 100)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    lens = [1400, 700, 1590, 30]
+    for l in range(4):
+        for b in range(4):
+            L.kv_import(kv, b, l, 0, *(torch.randn(lens[b], 128, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2)))
+    L.kv_set_len(kv, range(4), lens)
+    ids, n = [dev_i32([0, 1]), dev_i32([2, 3])], dev_i32([9, 9])
+    tokens = [dev_i32([synth.make_prompt(9, cfg["vocab"], 10 * i + j) for j in range(2)]) for i in range(2)]
+    want = [L.verify_step(m, kv, ids[i], tokens[i], n) for i, m in enumerate(models)]
+    streams = [torch.cuda.Stream() for _ in models]
+    out = [[torch.zeros_like(w) for _ in range(40)] for w in want]
+    torch.cuda.synchronize()
+    for r in range(40):
+        for i, m in enumerate(models):
+            L.verify_step(m, kv, ids[i], tokens[i], n, logits=out[i][r], stream=streams[i])
+    torch.cuda.synchronize()
+    for i, m in enumerate(models):
+        L.check(m)
+        assert all(torch.equal(x, want[i]) for x in out[i])
+
+
 def _calls_with_results(L):
     """Calls whose result the binding allocates: a call on a stream, by name."""
     cfg = synth.model_cfg("tiny", n_layers=1, d_model=64, d_ffn=64, vocab=64, n_heads=4, n_kv_heads=4, head_dim=64, max_draft=3)
