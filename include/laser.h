@@ -293,8 +293,9 @@ laser_status laser_kv_export(const laser_kv* kv, int32_t seq, int32_t layer, int
  * Rows that are not active are not read, cached or written.  rows * B <= 2^31 - 1 (prompts are
  * appended as rows too).  Asynchronous on `stream`.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim other than 64 and 128); found on the device and
- * reported by laser_kv_check, the sequence's rows then left out: INVALID_ARG (a bad sequence id or
- * parent; the rows behind a bad parent count their depth from it), CAPACITY (a sequence would outgrow its pages). */
+ * reported by laser_kv_check: INVALID_ARG (a bad sequence id) and CAPACITY (a sequence would outgrow its
+ * pages), the sequence's rows then left out; INVALID_ARG (a bad parent), its row and those behind it then
+ * count their depth from there. */
 laser_status laser_kv_append(laser_kv* kv, int32_t layer, const int32_t* seq_ids, const int32_t* parents,
                              const int32_t* n_rows, int32_t B, int32_t rows, int32_t dtype,
                              const void* q, int64_t q_stride, const void* k, int64_t k_stride,
@@ -312,7 +313,8 @@ laser_status laser_kv_append(laser_kv* kv, int32_t layer, const int32_t* seq_ids
  * rows of them are active.  It keeps partial results in memory of the cache's.  Asynchronous on `stream`.
  * Errors: INVALID_ARG (not a 4-bit cache among others), CAPACITY (B > 1024, or tiles of up to 40
  * rows x pages beyond 2^31 for a sequence or, of all, for an SM, or more tiles than 2^31); on the device
- * as above. */
+ * a bad sequence id and CAPACITY as above.  A bad parent, which laser_kv_append has reported, ends a
+ * row's path: it sees itself, what lies between, and the cached tokens. */
 laser_status laser_attend_int4(laser_kv* kv, int32_t layer, const int32_t* seq_ids, const int32_t* parents,
                                const int32_t* n_rows, int32_t B, int32_t rows, const void* q, int64_t q_stride,
                                void* out, int64_t out_stride, void* stream);
@@ -370,7 +372,8 @@ laser_status laser_profile_read(laser_model* m, int32_t cls, double* ms, int64_t
  * in fp32, the quotient as a product with 1 / repetition[b] and the last three terms as one number.
  *   logits, out  dev fp32[B, rows, V]; out may be logits itself (other overlaps are refused).  Rows that
  *            are not active are left as they are
- *   tokens, parents (or NULL), n_rows  as for laser_verify_step(_tree), rows = K + 1 <= 64
+ *   tokens, parents (or NULL), n_rows  as for laser_verify_step(_tree), rows = K + 1 <= 64; a parent that
+ *            is not an earlier row ends the path there
  *   hist, hist_len, hist_stride  the texts as laser_draft_temp takes them, pending token included
  *            (NULL: no text); prompt_len dev int32[B]: how much of each is prompt, which counts for the
  *            repetition penalty alone (NULL: all of it is generated)
