@@ -14,7 +14,7 @@
 // and of the splits.  So neither the other sequences matter, their lengths and rows, nor a row's place among drafts, and strict decoding equals
 // greedy decoding here, too.  All pages divided evenly over the SMs, whatever the lengths, with units cut anywhere, gave row results that
 // changed in the last bit with the neighbours; it was faster for ragged batches of long texts (one row over 64 texts of 4096 to 8192 tokens 100 us
-// instead of 115: a launch ends with CTAs of unequal length here) and for trees of 17 rows (121 instead of 129), and slower for few pages and
+// instead of 110: a launch ends with CTAs of unequal length here) and for trees of 17 rows (121 instead of 129), and slower for few pages and
 // for prompts (one row of 4 heads over 100 tokens 8.7 instead of 3.1; 32 rows of 32 prompts of up to 500 tokens, 32 heads, 53 instead of 42).
 //
 // What bounds it: the instructions.  A warp-level MMA of 16 x 8 x 16 keeps a scheduler from issuing for eight clocks; a page is 16 NT of
@@ -24,9 +24,9 @@
 // The softmax's reference m is a whole number in the exponent of two: raising it multiplies p and O by powers of two, exactly.  It is raised
 // only when a score exceeds it by more than 6, which a vote finds; p stays below 2^7, and bf16's and fp32's range is left to what is far below.
 //
-// Times (us; floors by bytes at 6.56 TB/s in brackets): 32 heads of 128, 9 rows over one text of 512 tokens 8.2 (0.4), over 16 of 256 to 768
-// 20.6 (6.7); 40 heads, trees of 17 rows over 64 texts of 256 to 1024 130 (42); 32 heads of 8 kv heads, one row over 64 texts of 4096 to 8192
-// 115 (77), 9 rows over one of 65536 55 (13).
+// Times (us; floors by bytes at 6.56 TB/s in brackets): 32 heads of 128, 9 rows over one text of 512 tokens 7.8 (0.4), over 16 of 256 to 768
+// 20.4 (6.7); 40 heads, trees of 17 rows over 64 texts of 256 to 1024 129 (42); 32 heads of 8 kv heads, one row over 64 texts of 4096 to 8192
+// 110 (77), 9 rows over one of 65536 52 (13).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -47,6 +47,7 @@ constexpr int kMostTiles = 5;      // of eight rows in a tile: O takes 80 regist
 constexpr int kWarps = 4;          // of a CTA
 constexpr int kRun = 2;            // blocks of a team in a run
 constexpr int kMostSplits = 256;   // CTAs that share a unit's pages
+constexpr int kLarge = 3;          // runs of a large one to a small one's
 constexpr int kMostWaves = 4;      // CTAs of a launch that splits pages, in what is resident
 
 // a unit that several CTAs have pieces of (count = 0: none)
@@ -91,6 +92,7 @@ struct AttnArgs {
   unsigned group_inv;                          // 2^32 / G rounded up (G > 1)
   float scale;                                 // log2(e) / sqrt(dh)
   int tiles, splits;                           // of a sequence and kv head: tiles; CTAs that share a tile's pages
+  int large, units;                            // those of them that have kLarge times the others' share; (sequence, kv head, tile) altogether
   float* records;                              // their pieces [unit][split]
   Join* joins;                                 // [unit]
   int32_t* status;
@@ -168,7 +170,7 @@ attn_int4_kernel(const AttnArgs a) {
   constexpr int OT = MT / S;             // a warp's
   constexpr int QC = DH / 32;            // 16-byte pieces of a lane's share of a Q row
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ unsigned long long s_path[64];         // token trees: the rows that a row of the sequence sees
+  __shared__ unsigned long long s_path[T][64];      // token trees: the rows that a row of the sequence sees
   __shared__ __align__(16) float2 s_ml[T][TM];      // m and sum of the rows of a team's piece
   __shared__ float s_half[S == 1 ? 1 : kWarps][TM];         // what a warp tells the other of its rows: highest scores, or sums
   __shared__ uint32_t s_high[S == 1 ? 1 : kWarps][4 * NT];  // and highest probabilities, of two rows
@@ -179,12 +181,18 @@ attn_int4_kernel(const AttnArgs a) {
 
   next_may_launch();
   // ---- the unit, and this CTA's share of its pages ----
-  const unsigned unit = blockIdx.x / unsigned(a.splits), split = blockIdx.x - unit * a.splits;
+  const unsigned split = blockIdx.x / unsigned(a.units), unit = blockIdx.x - split * a.units;
   const unsigned unit_hk = unit / unsigned(a.tiles), tile = unit - unit_hk * a.tiles;
   const int b = int(unit_hk / unsigned(a.Hkv)), hk = int(unit_hk - unsigned(b) * a.Hkv), row0 = int(tile) * TM;
-  // Blocks of S pages, in runs of kRun blocks a team: run j is split j % splits', its teams take the blocks in turn.
+  // Blocks of S pages, in runs of kRun blocks a team, whose teams take the blocks in turn.  Of every `cycle` runs the first splits, the large ones,
+  // have kLarge each, the others one.
   constexpr int kRunAll = kRun * T;
-  auto block_at = [&](int x) { return ((x / kRun) * a.splits + int(split)) * kRunAll + x % kRun * T + team; };      // the team's x-th
+  const int large = int(split) < a.large, cycle = a.splits + (kLarge - 1) * a.large;
+  const int first_run = large ? int(split) * kLarge : int(split) + (kLarge - 1) * a.large;
+  auto block_at = [&](int x) {        // the team's x-th
+    const int run = x / kRun, round = large ? run / kLarge : run;
+    return (round * cycle + first_run + (large ? run - round * kLarge : 0)) * kRunAll + x % kRun * T + team;
+  };
   // (the numbers of the first pages are on their way while the sequence's length is)
   const int32_t* table = a.page_table;
   int ids = -1;
@@ -216,24 +224,15 @@ attn_int4_kernel(const AttnArgs a) {
     }
   }
   const int nrows = nr * a.G, pages = (ctx + nr + 15) >> 4, blocks = (pages + S - 1) / S;
-  const int parts = nrows > row0 ? min(a.splits, (blocks + kRunAll - 1) / kRunAll) : 0;
+  const int runs = (blocks + kRunAll - 1) / kRunAll;
+  const int parts = nrows <= row0 ? 0 : runs <= kLarge * a.large ? (runs + kLarge - 1) / kLarge : min(a.splits, runs - (kLarge - 1) * a.large);
   if (a.splits > 1 && split == 0 && tid == 0) a.joins[unit] = Join{b, hk, row0, nrows, parts > 1 ? parts : 0};
   if (int(split) >= parts) return;
   auto blocks_of = [&](int w) {        // team w's
-    const int runs = blocks / kRunAll, rest = blocks - runs * kRunAll;
-    return kRun * ((runs - int(split) + a.splits - 1) / a.splits) + (runs % a.splits == int(split) ? max(rest - w + T - 1, 0) / T : 0);
+    const int whole = blocks / kRunAll, rounds = whole / cycle, ahead = whole - rounds * cycle - first_run, mine = large ? kLarge : 1;
+    return kRun * (rounds * mine + min(max(ahead, 0), mine)) + (ahead >= 0 && ahead < mine ? max(blocks - whole * kRunAll - w + T - 1, 0) / T : 0);
   };
   const int n = blocks_of(team);
-  if (a.parents) {
-    if (warp == 0) {
-      unsigned long long mask[2];
-      tree_paths(a.parents + size_t(b) * a.Rs, nr, lane, mask);
-      s_path[lane] = mask[0];
-      s_path[lane + 32] = mask[1];
-    }
-    __syncthreads();
-  }
-
   if (n > 0) {
     uint8_t* const region = smem + team * Z::kRegion;
     const uint32_t ring_at = smem_u32(region) + half * (ST * BLK) + lane * 16;
@@ -258,6 +257,13 @@ attn_int4_kernel(const AttnArgs a) {
       copies_end();
     }
 
+    if (a.parents && half == 0) {
+      unsigned long long mask[2];
+      tree_paths(a.parents + size_t(b) * a.Rs, nr, lane, mask);
+      s_path[team][lane] = mask[0];
+      s_path[team][lane + 32] = mask[1];
+      __syncwarp();
+    }
     // ---- Q: a lane's features are those of its K words ----
     uint32_t qa[Z::kQInSmem ? 1 : DH / 8];
     uint4* const my_q = reinterpret_cast<uint4*>(region + S * ST * BLK) + lane;
@@ -333,7 +339,7 @@ attn_int4_kernel(const AttnArgs a) {
           for (int y = 0; y < 2; ++y) {
             const int i = verify_row(min(row0 + 8 * t + 2 * qd + y, nrows - 1));      // (rows that are not active: as the last)
             if (a.parents) {
-              const unsigned long long see = s_path[i];
+              const unsigned long long see = s_path[team][i];
               if (rel0 >= 0 && (rel0 >= 64 || !(see >> (rel0 & 63) & 1))) x[t][y] = -INFINITY;
               if (rel1 >= 0 && (rel1 >= 64 || !(see >> (rel1 & 63) & 1))) x[t][2 + y] = -INFINITY;
             } else {
@@ -635,13 +641,22 @@ laser_status launch_attention(const laser_kv* kv, int n_heads, AttnArgs a, float
   auto launch = [&](auto dh, auto tiles_tag) -> laser_status {
     constexpr int DH = decltype(dh)::value, NT = decltype(tiles_tag)::value;
     using Z = Sizes<DH, NT>;
-    const int64_t resident = int64_t(kv->attn_sms) * Z::kCtas, runs = ceil_div(ceil_div(kv->pages_per_seq, Z::kTeam), kRun * Z::kTeams);
-    // CTAs for one wave; texts of several sequences may differ in length, and more CTAs than are resident even that out as long as each has
-    // pages enough
+    const int64_t resident = int64_t(kv->attn_sms) * Z::kCtas, runs = ceil_div(ceil_div(kv->pages_per_seq, Z::kTeam), kRun * Z::kTeams);      // (of a text as long as may be)
+    // As many CTAs as are resident, or less where that leaves each the same runs at most.  Texts of several sequences may differ in length: then
+    // more, as long as each has pages enough, the large ones first and small ones for the end (one row over 64 texts of 4096 to 8192: one CTA a
+    // unit 135 us, two 122, four of a size 116, two large and two small 110, eight of a size 118).
     const int64_t wave = resident / units, waves = a.B > 1 ? std::min<int64_t>(kMostWaves * resident / units, kv->pages_per_seq / 32) : 0;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({std::max(wave, waves), runs, kMostSplits})));
+    a.large = 0;
+    if (waves > std::max<int64_t>(wave, 1)) {
+      a.splits = int(std::min<int64_t>({waves, runs, kMostSplits}));
+      a.large = a.splits / 2;
+    } else {
+      a.splits = int(std::max<int64_t>(1, std::min<int64_t>({wave, runs, kMostSplits})));
+      a.splits = ceil_div(int(runs), ceil_div(int(runs), a.splits));
+    }
+    a.units = int(units);
     a.joins = reinterpret_cast<Join*>(a.records + size_t(units) * a.splits * Z::kRecord);
-    // (two tiles: four CTAs an SM take 128 registers a thread, which makes one slower: 16 texts of 256 to 768, 9 rows of 32 heads 20.8 us instead
+    // (two tiles: four CTAs an SM take 128 registers a thread, which makes one slower: 16 texts of 256 to 768, 9 rows of 32 heads, 20.8 us instead
     // of 23.2, one text of 512 9.7 instead of 8.3)
     constexpr int kFew = NT == 2 ? 3 : Z::kCtas;
     const dim3 grid(unsigned(units) * a.splits);

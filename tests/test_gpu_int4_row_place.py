@@ -19,9 +19,10 @@ def L():
     return binding
 
 
-# heads, kv heads, head_dim, sequences, rows, longest text: several CTAs a text, one, tiles of 8 to 40 rows, more than one tile
+# heads, kv heads, head_dim, sequences, rows, longest text: several CTAs a text, one, tiles of 8 to 40 rows, more than one tile; CTAs of two sizes
 SHAPES = [(4, 4, 64, 1, 1, 4000), (8, 2, 128, 3, 9, 3000), (32, 32, 128, 2, 9, 600), (32, 32, 128, 16, 9, 300), (40, 40, 128, 12, 17, 500), (8, 1, 64, 2, 5, 2000),
-          (4, 1, 128, 5, 33, 700), (2, 2, 64, 3, 64, 900), (4, 4, 64, 2, 41, 100), (8, 8, 64, 70, 3, 200)]
+          (4, 1, 128, 5, 33, 700), (2, 2, 64, 3, 64, 900), (4, 4, 64, 2, 41, 100), (8, 8, 64, 70, 3, 200), (32, 32, 64, 16, 1, 3000),
+          (16, 16, 64, 24, 9, 2100)]
 
 
 @pytest.mark.parametrize("heads,kv_heads,dim,B,rows,most", SHAPES)
