@@ -348,6 +348,8 @@ attn_int4_kernel(const AttnArgs a) {
             }
           }
       }
+      // (P enters the second product as bf16, in the numerator and in the sum, as in the attention over a bf16 cache: results are off by 0.0023 of
+      // their size where their own rounding to bf16 takes 0.0017; what the rounding leaves, as a second operand, would be that many MMAs again)
       // probabilities: from (token, row) to the second product's fragments, a row's tokens 2 qd, 2 qd + 1 (and 8 on) in lane g
       uint32_t p[NT][2];
       uint2* const team_p = reinterpret_cast<uint2*>(region + S * ST * BLK + Z::kQBytes + (it & 1) * Z::kPBytes) + lane;
