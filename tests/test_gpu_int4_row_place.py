@@ -66,6 +66,29 @@ def test_attention_of_a_row_anywhere(L, heads, kv_heads, dim, B, rows, most):
             assert torch.equal(left[b], full[b])
 
 
+def test_a_trees_rows_beside_other_trees(L):
+    """The rows of a token tree, where the other sequences have other trees, fewer rows, other lengths or none."""
+    rng = np.random.default_rng(8)
+    B, rows = 20, 17
+    kv = make(L, 8, 8, 128, B, 80)
+    lens = rng.integers(0, 1200, B)
+    for s in range(B):
+        L.kv_import(kv, s, 0, 0, bf(rng.standard_normal((lens[s] + rows, 1024)) * 2), bf(rng.standard_normal((lens[s] + rows, 1024))))
+    q = bf(rng.standard_normal((B, rows, 8, 128)) * 2)
+    par = lambda: np.array([[-1] + [rng.integers(0, i) for i in range(1, rows)] for _ in range(B)], np.int32)
+    first, ids = par(), dev_i32(range(B))
+    L.kv_set_len(kv, range(B), lens)
+    full = L.attend_int4(kv, 0, ids, dev_i32([rows] * B), q, parents=dev_i32(first))
+    for _ in range(4):
+        keep = rng.random(B) < 0.4
+        keep[0] = True
+        n = np.where(keep, rows, rng.integers(0, rows + 1, B))
+        L.kv_set_len(kv, range(B), np.where(keep, lens, rng.integers(0, 1200, B)))
+        got = L.attend_int4(kv, 0, ids, dev_i32(n), q, parents=dev_i32(np.where(keep[:, None], first, par())))
+        for b in np.nonzero(keep)[0]:
+            assert torch.equal(got[b], full[b])
+
+
 @pytest.mark.parametrize("over,B,K,ctx", [(dict(), 4, 8, 150), (dict(n_heads=4, n_kv_heads=2, head_dim=128, d_model=512), 3, 15, 700), (dict(), 40, 4, 61)])
 def test_a_step_of_all_rows_and_of_one_after_the_other(L, over, B, K, ctx):
     """Logits of all K + 1 rows at once, and of each alone: the same bits; what the cache then holds as well."""

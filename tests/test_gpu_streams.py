@@ -152,13 +152,14 @@ def test_results_belong_to_the_stream_of_the_call(L):
     flat = lambda r: [t for t in (r if isinstance(r, tuple) else (r,)) if t is not None]
     for name, call in _calls_with_results(L).items():
         want = [t.clone() for t in flat(call(None))]
-        torch.cuda.synchronize()
-        torch.cuda.empty_cache()
-        stale = [torch.empty_like(t) for t in want]
-        torch.cuda._sleep(40_000_000)                        # (some 20 ms)
-        for t in stale:
-            t.fill_(7)
-        del stale, t
-        got = flat(call(stream if name != "make_rows" else stream.cuda_stream))          # (a handle will do as well)
-        torch.cuda.synchronize()
-        assert all(torch.equal(a, b) for a, b in zip(got, want)), name
+        for s in (stream, stream.cuda_stream):               # (a handle will do as well)
+            torch.cuda.synchronize()
+            torch.cuda.empty_cache()
+            stale = [torch.empty_like(t) for t in want]
+            torch.cuda._sleep(40_000_000)                    # (some 20 ms)
+            for t in stale:
+                t.fill_(7)
+            del stale, t
+            got = flat(call(s))
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), name
